@@ -61,8 +61,18 @@ typedef enum {
                                     STAR_NOALLOC_SCRATCH_BYTES */
 } star_status;
 
-/* bits of the device-error word */
-enum { STAR_DEV_BAD_INST = 1, STAR_DEV_BAD_CUR = 2, STAR_DEV_BAD_REM = 4 };
+/* bits of the device-error word; the last four come from the cache's calls:
+ * a length or row range, a page index, a parent slot out of range, and too few
+ * free pages on an instance */
+enum {
+    STAR_DEV_BAD_INST = 1,
+    STAR_DEV_BAD_CUR = 2,
+    STAR_DEV_BAD_REM = 4,
+    STAR_DEV_BAD_LEN = 8,
+    STAR_DEV_BAD_PAGE = 16,
+    STAR_DEV_BAD_PARENT = 32,
+    STAR_DEV_NO_PAGES = 64
+};
 
 typedef enum { STAR_F32 = 0, STAR_BF16 = 1 } star_dtype;
 typedef enum { STAR_ACT_RELU = 0, STAR_ACT_GELU_ERF = 1 } star_act;
@@ -395,6 +405,150 @@ star_status star_plan_migrations(const star_plan_params* p, const int32_t* cur_l
                                  const int32_t* rem_len, int32_t* inst_of, int64_t* load,
                                  const uint16_t* beta, star_move* moves, int32_t* n_moves,
                                  void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * (g1) Pages of the key-value cache.
+ *
+ * What the load curves count and a migration moves: every request's keys and
+ * values lie in pages of page_size tokens, the same pages in every layer of
+ * one pool.  Layer y's page x is page_bytes bytes at
+ *     kv + y layer_stride + x page_stride;
+ * instance i owns pages i P .. i P + P - 1, P = n_pages / n_inst.  A request
+ * has a slot b: a row of the page table (table[b, j] holds its tokens
+ * j page_size ..), its length seq_len[b] and its instance seq_inst[b].
+ * refs[x] counts the rows that hold page x; 0 is a free page.  Table entries
+ * past ceil(seq_len / page_size) mean nothing and are neither read nor
+ * written.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int32_t n_seq;        /* slots >= 0 */
+    int32_t max_pages;    /* columns of the page table >= 1;
+                             max_pages * page_size <= 2^30 */
+    int32_t n_pages;      /* pages of the pool >= 1, a multiple of n_inst, <= 2^30 */
+    int32_t n_inst;       /* instances, 1 .. 1024 */
+    int32_t page_size;    /* tokens per page: a power of two, 16 .. 256 */
+    int32_t n_layers;     /* >= 1 */
+    int64_t page_bytes;   /* bytes of one page in one layer, a multiple of 16 */
+    int64_t page_stride;  /* bytes between pages, >= page_bytes, a multiple of 16 */
+    int64_t layer_stride; /* bytes between layers, a multiple of 16; the layers'
+                             pages must not overlap */
+} star_pages_params;
+
+/* Pages for every slot's next length: growth, truncation, release, forks and
+ * the migrations of a plan in one call, all as of the state on entry.
+ *   Slot b afterwards holds new_len[b] tokens on instance inst_of[b] (its own
+ * instance if inst_of is NULL; star_plan_migrations leaves the planned
+ * placement in the same form).  Its first keep = min(new_len[b], seq_len[a])
+ * tokens are those of slot a = parent[b] (b itself if parent is NULL; -1:
+ * none, keep = 0).  Of their pages,
+ *   - on the same instance the full ones become shared with a (each further
+ *     row that holds a page adds 1 to its count), and the partly filled one is
+ *     kept where a == b and its count is 1, else copied, so that the tokens to
+ *     come never go to a shared page;
+ *   - on another instance all are copied.
+ * Copies and further pages take the instance's pages that are free on entry,
+ * ascending, slots and then page positions ascending.  Pages given up serve
+ * later calls, not this one.
+ *   Slots that need free pages are served while the instance's running demand
+ * (over its slots in order, served or not) does not exceed its free pages;
+ * the others stay as they were and STAR_DEV_NO_PAGES is set (seq_len_out tells
+ * which).  So do slots with lengths, instances or parents out of range
+ * (STAR_DEV_BAD_LEN, _INST, _PARENT).  A page index out of range is neither
+ * counted nor copied (STAR_DEV_BAD_PAGE).
+ *   parent, new_len, inst_of: int32 [n_seq]; table: int32 [n_seq, max_pages];
+ *   seq_len: int32 [n_seq]; seq_inst: int32 [n_seq], or NULL where n_inst == 1;
+ *   refs: int32 [n_pages]; kv: the pool, 16-byte aligned, pages copied in place.
+ *   table_out, seq_len_out, seq_inst_out (may be NULL where n_inst == 1),
+ *   refs_out: the state afterwards.  Each may be its own input, except table_out where
+ *   parent is given; no other overlap is allowed. */
+size_t star_assign_pages_workspace_size(const star_pages_params* p);
+
+star_status star_assign_pages(const star_pages_params* p, const int32_t* parent,
+                              const int32_t* new_len, const int32_t* inst_of,
+                              const int32_t* table, const int32_t* seq_len,
+                              const int32_t* seq_inst, const int32_t* refs, void* kv,
+                              int32_t* table_out, int32_t* seq_len_out, int32_t* seq_inst_out,
+                              int32_t* refs_out, void* ws, size_t ws_bytes, void* stream);
+
+/* Every instance's live pages to its lowest indices: with n_live[i] pages of
+ * instance i in use, those from i P + n_live[i] on move, in order, into the
+ * free ones below, contents in all layers, counts and table entries with them.
+ *   table, seq_len, refs, kv: as above; table_out: int32 [n_seq, max_pages],
+ *   may be table itself; refs_out: int32 [n_pages], not refs itself;
+ *   n_live: int32 [n_inst] out. */
+size_t star_compact_pages_workspace_size(const star_pages_params* p);
+
+star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
+                               const int32_t* seq_len, const int32_t* refs, void* kv,
+                               int32_t* table_out, int32_t* refs_out, int32_t* n_live, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * (g2) Attention over the cache.
+ *
+ * One layer's step of a decode batch, whose last layer's output the predictor
+ * (a) reads.  kv is one layer of the pool above, a page being
+ * [2 (keys, values)][n_kv_heads][page_size][head_dim] of dtype.  Query head x
+ * reads key-value head x / (n_heads / n_kv_heads).  A query at position p of
+ * its request sees the keys at positions j <= p with
+ *     window == 0  or  j > p - window  or  j < sinks,
+ * and gives
+ *     out = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j exp(scale q . k_j)
+ * (natural logarithm; 0 and -infinity where nothing is visible).  What a row
+ * does not see does not change it, whatever it holds; pages that no row sees
+ * are not read, and their table entries mean nothing.
+ *   Both calls first store the new tokens: k_new and v_new are the keys and
+ * values of the last tokens of each request, which seq_len counts already
+ * (star_assign_pages made room).  The page that a request's new tokens go to
+ * must be its alone.
+ *   Precision: bf16 or fp32 operands, fp32 scores, softmax statistics and
+ * sums; the probabilities enter the second product as a bf16 hi/lo pair or as
+ * one bf16 (long prompts) for bf16, as fp32 for fp32; one rounding of out.
+ *   A request whose length or row range is out of range is left out, its rows
+ * of out and lse stay as they were (STAR_DEV_BAD_LEN); the tokens of a page
+ * index out of range are left out (STAR_DEV_BAD_PAGE).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int32_t n_seq;       /* slots >= 0 */
+    int32_t n_rows;      /* rows of q: n_seq (decode); all new tokens (prompt) */
+    int32_t n_heads;     /* query heads, a multiple of n_kv_heads */
+    int32_t n_kv_heads;  /* >= 1 */
+    int32_t head_dim;    /* 64, 128 or 256 */
+    int32_t dtype;       /* star_dtype of q, k_new, v_new, kv and out */
+    int32_t page_size;   /* a power of two, 16 .. 256 */
+    int32_t n_pages;     /* pages of the pool */
+    int32_t max_pages;   /* columns of the page table; max_pages * page_size <= 2^30 */
+    int32_t window;      /* >= 0; 0: none */
+    int32_t sinks;       /* >= 0 first tokens that stay visible under a window */
+    float   scale;       /* finite */
+    int64_t q_stride;    /* elements between rows of q (a multiple of 16 bytes) */
+    int64_t kv_stride;   /* elements between rows of k_new and of v_new (the same) */
+    int64_t page_stride; /* bytes between pages, a multiple of 16 */
+} star_attend_params;
+
+/* One new token a request.  q [n_seq, n_heads, head_dim], k_new and v_new
+ * [n_seq, n_kv_heads, head_dim], rows q_stride and kv_stride apart; out
+ * [n_seq, n_heads, head_dim] dense; lse fp32 [n_seq, n_heads] or NULL; table
+ * int32 [n_seq, max_pages], seq_len int32 [n_seq].  Slot b's token stands at
+ * position seq_len[b] - 1; a slot with seq_len 0 is empty: nothing is stored,
+ * its rows are 0 (lse -infinity).  All tensors 16-byte aligned (lse 4). */
+size_t star_attend_decode_workspace_size(const star_attend_params* p);
+
+star_status star_attend_decode(const star_attend_params* p, const void* q, const void* k_new,
+                               const void* v_new, void* kv, const int32_t* table,
+                               const int32_t* seq_len, void* out, float* lse, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* Several new tokens a request: q_start int32 [n_seq + 1] (ascending, at most
+ * n_rows) gives slot b rows q_start[b] .. q_start[b + 1] - 1 of q, k_new,
+ * v_new, out and lse; they are its last tokens, in order, and no more than
+ * seq_len[b].  Rows outside every range are left as they were. */
+size_t star_attend_prompt_workspace_size(const star_attend_params* p);
+
+star_status star_attend_prompt(const star_attend_params* p, const void* q, const void* k_new,
+                               const void* v_new, void* kv, const int32_t* table,
+                               const int32_t* seq_len, const int32_t* q_start, void* out,
+                               float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Housekeeping.

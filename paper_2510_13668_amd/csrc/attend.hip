@@ -1,0 +1,692 @@
+// Attention over the paged key-value cache (include/star.h, "attention over
+// the cache"): the row-block kernel behind star_attend_decode and short
+// star_attend_prompt calls, and the kernel that stores a prompt's new tokens.
+#include "star_common.hpp"
+#include "star_internal.hpp"
+
+namespace star {
+
+namespace {
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kRows = 16;        // query rows of one block (an MFMA's columns)
+constexpr int kThreads = 256;    // four waves share a block's keys
+constexpr int kWaves = kThreads / kWave;
+constexpr float kLn2 = 0.69314718055994531f;
+
+template <int kDtype> struct Elem;
+template <> struct Elem<STAR_BF16> {
+    static constexpr int kBytes = 2, kTile = 32;   // tokens of one tile: a product's K
+};
+template <> struct Elem<STAR_F32> {
+    static constexpr int kBytes = 4, kTile = 16;
+};
+
+// The keys that the rows at positions p0..p1 of one request can see, in tiles:
+// nA tiles of first tokens (sinks), then tiles b0.. up to p1's.
+struct Tiles {
+    int nA, b0, n;
+    __device__ int at(int u) const { return u < nA ? u : u - nA + b0; }
+};
+template <int kTile>
+__device__ inline Tiles tiles_of(const AttendArgs& a, int p0, int p1) {
+    Tiles t;
+    const int lo = a.window && p0 >= a.window ? p0 - a.window + 1 : 0;
+    t.b0 = lo / kTile;
+    const int s = a.window ? (a.sinks < p1 + 1 ? a.sinks : p1 + 1) : 0;
+    const int nA = (s + kTile - 1) / kTile;
+    t.nA = nA < t.b0 ? nA : t.b0;
+    t.n = p1 < 0 ? 0 : t.nA + p1 / kTile - t.b0 + 1;
+    return t;
+}
+
+// One request of the call: L cached tokens, the last T of them new, its rows
+// of q from row0 on.  A request that breaks a precondition has no rows.
+struct Slot {
+    int L, T, row0, blocks;   // blocks of kRows rows
+    int steps;                // scheduling steps of one block (kWaves tiles each)
+};
+template <int kTile>
+__device__ inline Slot slot_of(const AttendArgs& a, int b, int32_t& bad) {
+    Slot s;
+    s.L = a.seq_len[b];
+    bool ok = s.L >= 0 && s.L <= a.max_pages << a.ps_log2;
+    if (a.q_start) {
+        const int from = a.q_start[b], to = a.q_start[b + 1];
+        s.row0 = from;
+        s.T = to - from;
+        ok = ok && from >= 0 && to >= from && to <= a.n_rows && s.T <= s.L;
+    } else {
+        s.row0 = b;
+        s.T = 1;                       // an empty request's row is all zeros
+    }
+    if (!ok) {
+        bad |= STAR_DEV_BAD_LEN;
+        s.L = s.T = 0;
+    }
+    s.blocks = (int)(((int64_t)s.T * a.g + kRows - 1) / kRows);
+    int n = tiles_of<kTile>(a, s.L - 1, s.L - 1).n;
+    if (s.T > 1 && a.window) {          // a block's rows span at most kRows positions
+        const int all = (s.L - 1) / kTile + 1;
+        n = n + (kRows + kTile - 1) / kTile + 1;
+        n = n < all ? n : all;
+    }
+    s.steps = n > kWaves ? (n + kWaves - 1) / kWaves : 1;
+    return s;
+}
+
+// maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48: two register
+// swaps between rows of 16 lanes instead of LDS permutes
+__device__ inline float quad_max(float v) {
+    auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ inline float quad_sum(float v) {
+    auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// ---------------------------------------------------------------------------
+// One tile's keys and values in registers.
+//
+// With r = lane % 16 and c = lane / 16, the scores are the product
+// S^T [tokens x rows] = K Q^T, whose result gives lane (r, c) the tokens
+// 4c..4c+3 of each 16 for row r.  Those are the contraction slots that the
+// second product, O^T [d x rows] = V^T P^T, reads from lane (r, c), so the
+// probabilities never leave their lane.  V's rows are read whole (16 lanes one
+// row) and lane (r, c) holds d = r E .. r E + E - 1 of its tokens: tile i of
+// the second product takes element i of every lane.  No LDS in the loop.
+// ---------------------------------------------------------------------------
+template <int kDtype, int D>
+struct Tile {
+    static constexpr int kB = Elem<kDtype>::kBytes, kT = Elem<kDtype>::kTile;
+    static constexpr int kHalves = kT / 16;
+    static constexpr int E = D / 16;                    // d per lane
+    static constexpr int kRowV = E * kB;                // bytes of one lane's share of a V row
+    static constexpr int kRowsV = 4 * kHalves;          // V rows per lane
+    static constexpr int kChunks = D * kB / 64;         // 16-byte loads of one K row per lane
+    u32x4 k[kHalves][kChunks];
+    uint32_t v[kRowsV][kRowV / 4];
+};
+
+// where one 16-token half of a tile lies: its page (checked), or nowhere
+struct Half {
+    const char* base;     // the page's first byte of this head's keys, at the half's first token
+    bool ok;
+};
+
+template <int kDtype, int D>
+__device__ inline void load_row(const char* p, uint32_t* to) {
+    constexpr int n = Tile<kDtype, D>::kRowV;
+    if constexpr (n == 8) {
+        const u32x2 x = *(const u32x2*)p;
+        to[0] = x[0], to[1] = x[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < n / 16; ++i) {
+            const u32x4 x = *(const u32x4*)(p + 16 * i);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) to[4 * i + w] = x[w];
+        }
+    }
+}
+
+// the 16-byte pieces of a K row that lane (r, c) contracts: piece i of the
+// four lanes c = 0..3 is 64 consecutive bytes
+template <int kDtype, int D>
+__device__ inline void load_k(const char* row, int c, u32x4* to) {
+#pragma unroll
+    for (int i = 0; i < Tile<kDtype, D>::kChunks; ++i)
+        to[i] = *(const u32x4*)(row + i * 64 + c * 16);
+}
+
+// A product's result may be read a number of wait states after it is issued (11
+// for these shapes).  The compiler counts them within a basic block; where a
+// branch came between, it was seen to count the longer of two paths only
+// (fp32, 256 wide: the last product was missing from one register in four).
+// So results meet 16 wait states before any branch.
+__device__ inline void settle(f32x4& x) { asm volatile("s_nop 15" : "+v"(x)); }
+
+// S^T += K Q^T for one 16-token half
+template <int kDtype, int D>
+__device__ inline f32x4 scores(const u32x4* k, const u32x4* q) {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < Tile<kDtype, D>::kChunks; ++i) {
+        if constexpr (kDtype == STAR_BF16) {
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[i]),
+                                                        __builtin_bit_cast(bf16x8_t, q[i]), s, 0,
+                                                        0, 0);
+        } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[i][x]),
+                                                         __uint_as_float(q[i][x]), s, 0, 0, 0);
+        }
+    }
+    settle(s);
+    return s;
+}
+
+// O^T += V^T P^T for one tile; p[4 h + x] = lane (r, c)'s token 4c + x of half h.
+// bf16: P enters as a bf16 pair hi + lo (about 2^-17 relative): the products
+// are idle behind the loads, and one bf16 would add its 2^-9 to the output's.
+template <int kDtype, int D>
+__device__ inline void accumulate(const uint32_t (&v)[Tile<kDtype, D>::kRowsV]
+                                                     [Tile<kDtype, D>::kRowV / 4],
+                                  const float* p, f32x4* o) {
+    if constexpr (kDtype == STAR_BF16) {
+        u32x4 hi, lo;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            uint32_t h, l;
+            split_bf16x2(p[2 * x], p[2 * x + 1], h, l);
+            hi[x] = h, lo[x] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            u32x4 a;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)     // element i of rows 2x and 2x + 1
+                a[x] = __builtin_amdgcn_perm(v[2 * x + 1][i / 2], v[2 * x][i / 2],
+                                             i & 1 ? 0x07060302u : 0x05040100u);
+            const bf16x8_t va = __builtin_bit_cast(bf16x8_t, a);
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, hi),
+                                                           o[i], 0, 0, 0);
+            o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8_t, lo),
+                                                           o[i], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[x][i]), p[x], o[i],
+                                                            0, 0, 0);
+    }
+    settle(o[D / 16 - 1]);          // the last one issued
+}
+
+template <int kDtype>
+__device__ inline bool not_finite(uint32_t w) {
+    if constexpr (kDtype == STAR_F32)
+        return (w & 0x7F800000u) == 0x7F800000u;
+    else
+        return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+}
+
+// the larger magnitudes, value by value (and the signs dropped)
+template <int kDtype>
+__device__ inline uint32_t larger(uint32_t a, uint32_t w) {
+    if constexpr (kDtype == STAR_F32) return max(a, w & 0x7FFFFFFFu);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+                                            __builtin_bit_cast(u16x2, a),
+                                            __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
+}
+// the word with its values that are not finite at 0
+template <int kDtype>
+__device__ inline uint32_t finite_part(uint32_t w) {
+    if constexpr (kDtype == STAR_F32) return not_finite<kDtype>(w) ? 0u : w;
+    const uint32_t lo = (w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu;
+    const uint32_t hi = (w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u;
+    return lo | hi;
+}
+template <int kDtype>
+__device__ inline float value_at(const uint32_t* w, int i) {
+    if constexpr (kDtype == STAR_F32) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+}
+
+// ---------------------------------------------------------------------------
+// The row-block kernel: any lengths, group sizes, masks and both types.
+//
+// A block is up to 16 (new token, query head) rows of one request that share a
+// key-value head; its keys go by in tiles, one tile per wave and step, with
+// the running maximum and sum of the softmax.  All blocks' steps in a row are
+// cut into equal pieces, one per workgroup, whatever the requests' lengths: a
+// piece ends inside a long cache or spans several short ones.  A block cut
+// between workgroups leaves its parts (maximum, sum, unnormalised output) in
+// the workspace, and the last of them to arrive joins all in order, so results
+// do not depend on the order of arrival.  Keys and values are read once (16
+// rows or fewer a head), registers to registers; HBM bounds it.
+// ---------------------------------------------------------------------------
+template <int kDtype, int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
+    using TT = Tile<kDtype, D>;
+    constexpr int kB = TT::kB, kT = TT::kT, E = TT::E;
+    constexpr bool kAhead = D * kB < 1024;
+    constexpr int kPart = kRows * D + 4 * kRows;       // floats of one part
+    __shared__ float s_o[kWaves][kRows][D + 4];
+    __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+    __shared__ int64_t s_tmp[kWaves + 1], s_base;
+    __shared__ int s_b;
+    __shared__ uint32_t s_ticket;
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int r = lane & 15, c = lane >> 4;
+    const int wg = blockIdx.x;
+
+    // this workgroup's piece of all steps
+    const int per = (a.n_seq + kThreads - 1) / kThreads;
+    int32_t bad = 0;
+    int64_t mine = 0, total;
+    for (int b = tid * per; b < min(a.n_seq, (tid + 1) * per); ++b) {
+        const Slot s = slot_of<kT>(a, b, bad);
+        mine += (int64_t)a.n_kv * s.blocks * s.steps;
+    }
+    if (wg == 0) report_error(a.err, bad);
+    const int64_t before = block_exclusive_scan_i64<kThreads>(mine, OpAdd(), 0, s_tmp, &total);
+    const int64_t piece = max((int64_t)a.min_steps, ceil_div(total, gridDim.x));
+    int64_t u = wg * piece;
+    if (u >= total) return;
+    const int64_t end = min(total, u + piece);
+    if (before <= u && u < before + mine) {
+        int64_t base = before;
+        for (int b = tid * per;; ++b) {
+            const Slot s = slot_of<kT>(a, b, bad);
+            const int64_t n = (int64_t)a.n_kv * s.blocks * s.steps;
+            if (u < base + n) {
+                s_b = b;
+                s_base = base;
+                break;
+            }
+            base += n;
+        }
+    }
+    __syncthreads();
+    int b = __builtin_amdgcn_readfirstlane(s_b);
+    int64_t base = readlane_i64(s_base, 0);
+    int32_t err = 0;
+
+    const __amdgpu_buffer_rsrc_t part =
+        xch_rsrc(a.part, (uint32_t)(2 * gridDim.x * kPart * sizeof(float)));
+    while (u < end) {
+        Slot s = slot_of<kT>(a, b, bad);
+        int64_t n_slot = (int64_t)a.n_kv * s.blocks * s.steps;
+        while (u >= base + n_slot) {
+            base += n_slot;
+            s = slot_of<kT>(a, ++b, bad);
+            n_slot = (int64_t)a.n_kv * s.blocks * s.steps;
+        }
+        const int item = (int)((u - base) / s.steps);
+        const int64_t item_u = base + (int64_t)item * s.steps;
+        const int step0 = (int)(u - item_u);
+        const int steps = (int)min((int64_t)(s.steps - step0), end - u);
+        const int head = item / s.blocks, row_from = (item - head * s.blocks) * kRows;
+        const int rows = min(s.T * a.g - row_from, kRows);
+
+        // lane (r, c)'s row: its query and the position it stands at
+        const int first = s.L - s.T;                     // position of the first new token
+        const int row = row_from + r;
+        const bool live = r < rows && s.L > 0;
+        const int pos = live ? first + row / a.g : -1;
+        const int p0 = first + row_from / a.g;
+        const int p1 = first + (row_from + rows - 1) / a.g;
+        const int64_t q_row = s.row0 + row / a.g;
+        const int q_head = head * a.g + row % a.g;
+        u32x4 q[TT::kChunks];
+        if (live) {
+            load_k<kDtype, D>(a.q + q_row * a.q_stride + (int64_t)q_head * D * kB, c, q);
+        } else {
+#pragma unroll
+            for (int i = 0; i < TT::kChunks; ++i) q[i] = u32x4{0, 0, 0, 0};
+        }
+
+        const Tiles tl = tiles_of<kT>(a, p0, s.L > 0 ? p1 : -1);
+        const int32_t* pages = a.table + (int64_t)b * a.max_pages;
+        const char* kn = a.kn ? a.kn + (int64_t)b * a.kv_stride + (int64_t)head * D * kB : nullptr;
+        const char* vn = a.kn ? a.vn + (int64_t)b * a.kv_stride + (int64_t)head * D * kB : nullptr;
+        const int64_t v_off = (int64_t)a.n_kv * D * kB << a.ps_log2;   // values after keys
+
+        // where half h of tile t lies; a half that no row of the block sees is
+        // not looked up (its page may be gone), and a bad page is left out
+        auto half_at = [&](int t, int h) {
+            Half x;
+            const int j = t * kT + h * 16;
+            const bool seen = j <= p1 && (!a.window || j + 15 > p0 - a.window || j < a.sinks);
+            int page = 0;
+            if (seen) page = pages[j >> a.ps_log2];
+            page = __builtin_amdgcn_readfirstlane(page);
+            x.ok = seen && (uint32_t)page < (uint32_t)a.n_pages;
+            if (seen && !x.ok) err |= STAR_DEV_BAD_PAGE;
+            const int in = j & ((1 << a.ps_log2) - 1);
+            x.base = a.kv + (int64_t)(x.ok ? page : 0) * a.page_stride +
+                     (((int64_t)head << a.ps_log2) + in) * (D * kB);
+            return x;
+        };
+        auto load = [&](int t, TT& f, Half (&hf)[TT::kHalves]) {
+#pragma unroll
+            for (int h = 0; h < TT::kHalves; ++h) {
+                hf[h] = half_at(t, h);
+                const char* kb = hf[h].base + r * (D * kB);
+                const char* vb = hf[h].base + v_off + c * 4 * (D * kB) + r * TT::kRowV;
+                // the call's new token comes from its own arrays: the cache is
+                // written beside, and no one reads it there
+                const int at = a.kn ? s.L - 1 - (t * kT + h * 16) : -1;
+                if ((uint32_t)at < 16u) {
+                    load_k<kDtype, D>(r == at ? kn : kb, c, f.k[h]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        load_row<kDtype, D>(4 * c + x == at ? vn + r * TT::kRowV
+                                                            : vb + x * (D * kB),
+                                            f.v[4 * h + x]);
+                } else {
+                    load_k<kDtype, D>(kb, c, f.k[h]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        load_row<kDtype, D>(vb + x * (D * kB), f.v[4 * h + x]);
+                }
+            }
+        };
+
+        f32x4 o[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float m = -INFINITY, l = 0.0f;                   // l: this lane's tokens only
+
+        const int t_end = min(tl.n, kWaves * (step0 + steps));
+        int t = kWaves * step0 + wave;
+        TT f;
+        Half hf[TT::kHalves];
+        if (t < t_end) load(tl.at(t), f, hf);
+        for (; t < t_end; t += kWaves) {
+            TT nf;
+            Half nh[TT::kHalves];
+            if (kAhead && t + kWaves < t_end) load(tl.at(t + kWaves), nf, nh);
+
+            const int j0 = tl.at(t) * kT;
+            float p[4 * TT::kHalves];
+#pragma unroll
+            for (int h = 0; h < TT::kHalves; ++h) {
+                const f32x4 z = scores<kDtype, D>(f.k[h], q);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) p[4 * h + x] = z[x] * a.scale_log2;
+            }
+            // hidden keys: only where the tile is not visible to every row
+            bool all = j0 + kT - 1 <= p0 && rows == kRows;
+            all = all && (!a.window || j0 > p1 - a.window || j0 + kT <= a.sinks);
+#pragma unroll
+            for (int h = 0; h < TT::kHalves; ++h) all = all && hf[h].ok;
+            auto sees = [&](int j, int at, bool ok) {
+                return ok && j <= at && (!a.window || j > at - a.window || j < a.sinks);
+            };
+            if (!all) {
+#pragma unroll
+                for (int h = 0; h < TT::kHalves; ++h)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int j = j0 + 16 * h + 4 * c + x;
+                        if (!sees(j, pos, hf[h].ok)) p[4 * h + x] = -INFINITY;
+                        // values that no row sees may be anything: 0 there
+                        const bool any = hf[h].ok && j <= p1 &&
+                                         (!a.window || j > p0 - a.window || j < a.sinks);
+#pragma unroll
+                        for (int w = 0; w < TT::kRowV / 4; ++w)
+                            if (!any) f.v[4 * h + x][w] = 0;
+                    }
+            }
+            // the tile's largest magnitude tells whether all values are finite
+            uint32_t big = 0;
+#pragma unroll
+            for (int x = 0; x < TT::kRowsV; ++x)
+#pragma unroll
+                for (int w = 0; w < TT::kRowV / 4; ++w) big = larger<kDtype>(big, f.v[x][w]);
+
+            float top = p[0];
+#pragma unroll
+            for (int x = 1; x < 4 * TT::kHalves; ++x) top = fmaxf(top, p[x]);
+            top = fmaxf(m, quad_max(top));
+            const float ref = top == -INFINITY ? 0.0f : top;   // nothing seen yet: all p are 0
+            if (__any(top > m)) {
+                const float f_old = __builtin_amdgcn_exp2f(m - ref);
+                l *= f_old;
+#pragma unroll
+                for (int i = 0; i < E; ++i) o[i] *= f_old;
+            }
+            m = top;
+#pragma unroll
+            for (int x = 0; x < 4 * TT::kHalves; ++x) {
+                p[x] = __builtin_amdgcn_exp2f(p[x] - ref);
+                l += p[x];
+            }
+            // A value that is not finite would reach rows that do not see it as
+            // 0 times infinity, and the rows that do as infinity times hi + lo
+            // of unlike signs: such values leave the product and are added to
+            // the rows that see them (their probabilities are positive)
+            const bool fix = __any(not_finite<kDtype>(big));
+            if (fix) {
+                uint32_t* raw = (uint32_t*)&s_o[wave][0][0];     // [kT][D], as loaded
+#pragma unroll
+                for (int h = 0; h < TT::kHalves; ++h)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int w = 0; w < TT::kRowV / 4; ++w) {
+                            uint32_t& v = f.v[4 * h + x][w];
+                            raw[((16 * h + 4 * c + x) * D + r * E) * kB / 4 + w] = v;
+                            v = finite_part<kDtype>(v);
+                        }
+            }
+            accumulate<kDtype, D>(f.v, p, o);
+            if (fix) {
+                const uint32_t* raw = (const uint32_t*)&s_o[wave][0][0];
+                for (int j = 0; j < kT; ++j) {
+                    if (!sees(j0 + j, pos, j < 16 ? hf[0].ok : hf[TT::kHalves - 1].ok)) continue;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            const float v = value_at<kDtype>(raw, j * D + (4 * c + x) * E + i);
+                            if (!(fabsf(v) < INFINITY)) o[i][x] += v;
+                        }
+                }
+            }
+
+            if (kAhead) {
+                f = nf;
+#pragma unroll
+                for (int h = 0; h < TT::kHalves; ++h) hf[h] = nh[h];
+            } else if (t + kWaves < t_end) {
+                load(tl.at(t + kWaves), f, hf);
+            }
+        }
+
+        // the new token joins the cache, once per key-value head: by the wave
+        // of the block's last tile, where that tile is in this piece
+        if (a.kn && s.L > 0 && row_from == 0) {
+            const int last = tl.n - 1;
+            if (last % kWaves == wave && last / kWaves >= step0 && last / kWaves < step0 + steps) {
+                const int j = s.L - 1;
+                const int page = __builtin_amdgcn_readfirstlane(pages[j >> a.ps_log2]);
+                if ((uint32_t)page < (uint32_t)a.n_pages && lane < D * kB / 16) {
+                    char* to = a.kv + (int64_t)page * a.page_stride +
+                               (((int64_t)head << a.ps_log2) + (j & ((1 << a.ps_log2) - 1))) *
+                                   (D * kB) +
+                               lane * 16;
+                    *(u32x4*)to = *(const u32x4*)(kn + lane * 16);
+                    *(u32x4*)(to + v_off) = *(const u32x4*)(vn + lane * 16);
+                }
+            }
+        }
+
+        // the four waves' parts meet: thread (row, 16 of them) sums E outputs
+        l = quad_sum(l);
+        if (c == 0) s_m[wave][r] = m, s_l[wave][r] = l;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < E; ++i) s_o[wave][r][(4 * c + x) * E + i] = o[i][x];
+        __syncthreads();
+        const int jr = tid / 16, jd = (tid & 15) * E;
+        float jm = s_m[0][jr], jl = 0.0f, jo[E];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) jm = fmaxf(jm, s_m[w][jr]);
+        float jref = jm == -INFINITY ? 0.0f : jm;
+#pragma unroll
+        for (int i = 0; i < E; ++i) jo[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f_w = __builtin_amdgcn_exp2f(s_m[w][jr] - jref);
+            jl += f_w * s_l[w][jr];
+#pragma unroll
+            for (int i = 0; i < E; ++i) jo[i] += f_w * s_o[w][jr][jd + i];
+        }
+
+        bool write = true;
+        if (steps < s.steps) {
+            // a part of a block: its place goes by the workgroup that holds it
+            // (the block's first part after that workgroup's own first)
+            const int w0 = (int)(item_u / piece), w1 = (int)((item_u + s.steps - 1) / piece);
+            auto part_at = [&](int w) {
+                return (uint32_t)((2 * w + (w == w0)) * kPart * sizeof(float));
+            };
+            const uint32_t off = part_at(wg);
+            if ((tid & 15) == 0)
+                xch_store(u32x4{__float_as_uint(jm), __float_as_uint(jl), 0, 0}, part,
+                          off + jr * 16);
+            // (maximum and sum take the 16 bytes of two floats each and padding)
+#pragma unroll
+            for (int i = 0; i < E; i += 4)
+                xch_store(u32x4{__float_as_uint(jo[i]), __float_as_uint(jo[i + 1]),
+                                __float_as_uint(jo[i + 2]), __float_as_uint(jo[i + 3])},
+                          part, off + kRows * 16 + (jr * D + jd + i) * 4);
+            xch_wait_stores();
+            write = xch_last_arrival(a.tickets + w0, (uint32_t)(w1 - w0 + 1), &s_ticket);
+            if (write) {
+                jm = -INFINITY, jl = 0.0f;
+#pragma unroll
+                for (int i = 0; i < E; ++i) jo[i] = 0.0f;
+                for (int w = w0; w <= w1; ++w) {
+                    const uint32_t at = part_at(w);
+                    const u32x4 ml = xch_load(part, at + jr * 16);
+                    u32x4 v[E / 4];
+#pragma unroll
+                    for (int i = 0; i < E; i += 4)
+                        v[i / 4] = xch_load(part, at + kRows * 16 + (jr * D + jd + i) * 4);
+                    const float pm = __uint_as_float(ml[0]), pl = __uint_as_float(ml[1]);
+                    const float nm = fmaxf(jm, pm);
+                    jref = nm == -INFINITY ? 0.0f : nm;
+                    const float f0 = __builtin_amdgcn_exp2f(jm - jref);
+                    const float f1 = __builtin_amdgcn_exp2f(pm - jref);
+                    jm = nm;
+                    jl = jl * f0 + pl * f1;
+#pragma unroll
+                    for (int i = 0; i < E; ++i)
+                        jo[i] = jo[i] * f0 + __uint_as_float(v[i / 4][i & 3]) * f1;
+                }
+            }
+        }
+        if (write && jr < rows) {
+            const int wr = row_from + jr;
+            const int64_t at = (int64_t)(s.row0 + wr / a.g) * a.n_heads + head * a.g + wr % a.g;
+            const float inv = jl == 0.0f ? 0.0f : 1.0f / jl;   // a row that sees nothing is 0
+            char* to = a.out + (at * D + jd) * kB;
+            if constexpr (kDtype == STAR_BF16) {
+#pragma unroll
+                for (int i = 0; i < E; i += 4) {
+                    u32x2 x;
+                    x[0] = pack_bf16x2_rne(jo[i] * inv, jo[i + 1] * inv);
+                    x[1] = pack_bf16x2_rne(jo[i + 2] * inv, jo[i + 3] * inv);
+                    *(u32x2*)(to + i * kB) = x;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; i += 4)
+                    *(f32x4*)(to + i * kB) =
+                        f32x4{jo[i] * inv, jo[i + 1] * inv, jo[i + 2] * inv, jo[i + 3] * inv};
+            }
+            if (a.lse && (tid & 15) == 0)
+                a.lse[at] = jl == 0.0f ? -INFINITY : (jm + __builtin_amdgcn_logf(jl)) * kLn2;
+        }
+        __syncthreads();                                  // s_o is free for the next block
+        u += steps;
+    }
+    if (err && lane == 0) report_error(a.err, err);
+}
+
+// ---------------------------------------------------------------------------
+// The new tokens of prompts into their pages: one workgroup per token, 16
+// bytes a thread.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes) {
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+        // the request whose rows hold this one: the last that starts at or before it
+        int lo = 0, hi = a.n_seq;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.q_start[mid] <= row) lo = mid + 1;
+            else hi = mid;
+        }
+        const int b = lo - 1;
+        if (b < 0) continue;
+        const int from = a.q_start[b], to = a.q_start[b + 1], L = a.seq_len[b];
+        if (from < 0 || row >= to || to > a.n_rows || L < 0 || L > a.max_pages << a.ps_log2 ||
+            to - from > L)
+            continue;
+        const int j = (int)(L - (to - from) + (row - from));
+        const int page = a.table[(int64_t)b * a.max_pages + (j >> a.ps_log2)];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+        const int in = j & ((1 << a.ps_log2) - 1);
+        const int all = a.n_kv * row_bytes;               // bytes of one token's keys
+        char* base = a.kv + (int64_t)page * a.page_stride;
+        for (int x = threadIdx.x * 16; x < 2 * all; x += kThreads * 16) {
+            const int y = x < all ? x : x - all;
+            const int head = y / row_bytes, d = y - head * row_bytes;
+            const char* src = (x < all ? a.kn : a.vn) + row * a.kv_stride + y;
+            char* dst = base + ((int64_t)((x < all ? 0 : a.n_kv) + head) << a.ps_log2) * row_bytes +
+                        (int64_t)in * row_bytes + d;
+            *(u32x4*)dst = *(const u32x4*)src;
+        }
+    }
+}
+
+template <int kDtype, int D>
+hipError_t launch_rows(const AttendArgs& a, int grid, hipStream_t stream) {
+    hipLaunchKernelGGL((attend_rows_kernel<kDtype, D>), dim3(grid), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+AttendPlan plan_attend(const star_attend_params& p, bool decode) {
+    AttendPlan pl;
+    // two workgroups a CU (one where a row's 256 elements fill the registers)
+    pl.grid = p.head_dim == 256 ? 256 : 512;
+    static_assert(512 <= kMaxTickets, "one ticket per workgroup");
+    pl.min_steps = 2;
+    pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
+    (void)decode;
+    return pl;
+}
+
+hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype, int head_dim,
+                         hipStream_t stream) {
+    AttendArgs a = args;
+    a.min_steps = pl.min_steps;
+    if (a.n_seq == 0 || a.n_rows == 0) return hipSuccess;
+    if (a.q_start && a.kn) {
+        const int e = dtype == STAR_BF16 ? 2 : 4;
+        const int grid = a.n_rows < 4096 ? a.n_rows : 4096;
+        hipLaunchKernelGGL(store_tokens_kernel, dim3(grid), dim3(kThreads), 0, stream, a,
+                           head_dim * e);
+        hipError_t e1 = hipGetLastError();
+        if (e1 != hipSuccess) return e1;
+        a.kn = a.vn = nullptr;
+    }
+    if (dtype == STAR_BF16) {
+        if (head_dim == 64) return launch_rows<STAR_BF16, 64>(a, pl.grid, stream);
+        if (head_dim == 128) return launch_rows<STAR_BF16, 128>(a, pl.grid, stream);
+        return launch_rows<STAR_BF16, 256>(a, pl.grid, stream);
+    }
+    if (head_dim == 64) return launch_rows<STAR_F32, 64>(a, pl.grid, stream);
+    if (head_dim == 128) return launch_rows<STAR_F32, 128>(a, pl.grid, stream);
+    return launch_rows<STAR_F32, 256>(a, pl.grid, stream);
+}
+
+}  // namespace star

@@ -477,6 +477,179 @@ STAR_API star_status star_plan_migrations(const star_plan_params* p, const int32
 }
 
 // ---------------------------------------------------------------------------
+// pages of the cache
+// ---------------------------------------------------------------------------
+static bool page_size_ok(int32_t n) { return n >= 16 && n <= 256 && (n & (n - 1)) == 0; }
+
+static star_status check_pages_params(const star_pages_params* p) {
+    if (!p) return STAR_ERR_INVALID_ARG;
+    if (p->n_seq < 0 || p->max_pages < 1 || p->n_pages < 1 || p->n_inst < 1 || p->n_layers < 1 ||
+        p->page_bytes < 1 || p->page_size < 1)
+        return STAR_ERR_INVALID_ARG;
+    if (p->n_pages % p->n_inst) return STAR_ERR_INVALID_ARG;
+    if (!page_size_ok(p->page_size) || p->n_inst > 1024 || p->n_pages > 1 << 30)
+        return STAR_ERR_UNSUPPORTED;
+    if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return STAR_ERR_UNSUPPORTED;
+    if (p->page_bytes % 16 || p->page_stride % 16 || p->layer_stride % 16)
+        return STAR_ERR_UNSUPPORTED;
+    // the farthest byte of the pool has to fit 62 bits
+    if (p->page_stride < p->page_bytes || p->layer_stride < 0 ||
+        (p->n_layers > 1 && p->layer_stride < p->page_bytes))
+        return STAR_ERR_INVALID_ARG;
+    const __int128 far = (__int128)p->page_stride * p->n_pages +
+                         (__int128)p->layer_stride * p->n_layers;
+    if (far >= (__int128)1 << 62) return STAR_ERR_OVERFLOW;
+    return STAR_OK;
+}
+
+STAR_API size_t star_assign_pages_workspace_size(const star_pages_params* p) {
+    if (check_pages_params(p) != STAR_OK) return 0;
+    return plan_pages(*p).total;
+}
+
+STAR_API star_status star_assign_pages(const star_pages_params* p, const int32_t* parent,
+                                       const int32_t* new_len, const int32_t* inst_of,
+                                       const int32_t* table, const int32_t* seq_len,
+                                       const int32_t* seq_inst, const int32_t* refs, void* kv,
+                                       int32_t* table_out, int32_t* seq_len_out,
+                                       int32_t* seq_inst_out, int32_t* refs_out, void* ws,
+                                       size_t ws_bytes, void* stream) {
+    star_status st = check_pages_params(p);
+    if (st != STAR_OK) return st;
+    if (!refs || !kv || !refs_out) return STAR_ERR_INVALID_ARG;
+    if (p->n_seq > 0 && (!new_len || !table || !seq_len || !table_out || !seq_len_out))
+        return STAR_ERR_INVALID_ARG;
+    if (p->n_seq > 0 && p->n_inst > 1 && (!seq_inst || !seq_inst_out)) return STAR_ERR_INVALID_ARG;
+    if (parent && table_out == table && p->n_seq > 0) return STAR_ERR_INVALID_ARG;
+    if (!aligned(kv, 16)) return STAR_ERR_UNSUPPORTED;
+    const PagesPlan pl = plan_pages(*p);
+    st = check_ws(ws, ws_bytes, pl.total);
+    if (st != STAR_OK) return st;
+    hipError_t e = launch_assign(*p, pl, parent, new_len, inst_of, table, seq_len, seq_inst, refs,
+                                 kv, table_out, seq_len_out, seq_inst_out, refs_out, (char*)ws,
+                                 (hipStream_t)stream);
+    return e == hipSuccess ? STAR_OK : STAR_ERR_HIP;
+}
+
+STAR_API size_t star_compact_pages_workspace_size(const star_pages_params* p) {
+    if (check_pages_params(p) != STAR_OK) return 0;
+    return plan_pages(*p).total;
+}
+
+STAR_API star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
+                                        const int32_t* seq_len, const int32_t* refs, void* kv,
+                                        int32_t* table_out, int32_t* refs_out, int32_t* n_live,
+                                        void* ws, size_t ws_bytes, void* stream) {
+    star_status st = check_pages_params(p);
+    if (st != STAR_OK) return st;
+    if (!refs || !kv || !refs_out || !n_live || refs_out == refs) return STAR_ERR_INVALID_ARG;
+    if (p->n_seq > 0 && (!table || !seq_len || !table_out)) return STAR_ERR_INVALID_ARG;
+    if (!aligned(kv, 16)) return STAR_ERR_UNSUPPORTED;
+    const PagesPlan pl = plan_pages(*p);
+    st = check_ws(ws, ws_bytes, pl.total);
+    if (st != STAR_OK) return st;
+    hipError_t e = launch_compact(*p, pl, table, seq_len, refs, kv, table_out, refs_out, n_live,
+                                  (char*)ws, (hipStream_t)stream);
+    return e == hipSuccess ? STAR_OK : STAR_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+// attention over the cache
+// ---------------------------------------------------------------------------
+static star_status check_attend_params(const star_attend_params* p) {
+    if (!p) return STAR_ERR_INVALID_ARG;
+    if (p->n_seq < 0 || p->n_rows < 0 || p->n_heads < 1 || p->n_kv_heads < 1 || p->head_dim < 1 ||
+        p->page_size < 1 || p->n_pages < 1 || p->max_pages < 1 || p->window < 0 || p->sinks < 0)
+        return STAR_ERR_INVALID_ARG;
+    if (p->dtype != STAR_F32 && p->dtype != STAR_BF16) return STAR_ERR_INVALID_ARG;
+    if (p->n_heads % p->n_kv_heads || !isfinite(p->scale)) return STAR_ERR_INVALID_ARG;
+    const int64_t e = p->dtype == STAR_BF16 ? 2 : 4;
+    const __int128 page = (__int128)2 * p->n_kv_heads * p->page_size * p->head_dim * e;
+    if (p->q_stride < (int64_t)p->n_heads * p->head_dim ||
+        p->kv_stride < (int64_t)p->n_kv_heads * p->head_dim || p->page_stride < page)
+        return STAR_ERR_INVALID_ARG;
+    if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return STAR_ERR_UNSUPPORTED;
+    if (!page_size_ok(p->page_size)) return STAR_ERR_UNSUPPORTED;
+    if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return STAR_ERR_UNSUPPORTED;
+    if (p->q_stride * e % 16 || p->kv_stride * e % 16 || p->page_stride % 16)
+        return STAR_ERR_UNSUPPORTED;
+    // rows (token, head) are counted in 32 bits, bytes in 62
+    if ((int64_t)p->n_rows * p->n_heads >= (int64_t)1 << 31) return STAR_ERR_OVERFLOW;
+    const __int128 far = (__int128)p->page_stride * p->n_pages +
+                         ((__int128)p->q_stride + p->kv_stride) * p->n_rows * e;
+    if (far >= (__int128)1 << 62) return STAR_ERR_OVERFLOW;
+    return STAR_OK;
+}
+
+static size_t attend_bytes(const AttendPlan& pl) {
+    return STAR_WS_HEADER_BYTES + align_up(pl.part_bytes, 256);
+}
+
+static star_status attend(const star_attend_params* p, const void* q, const void* k_new,
+                          const void* v_new, void* kv, const int32_t* table,
+                          const int32_t* seq_len, const int32_t* q_start, bool decode, void* out,
+                          float* lse, void* ws, size_t ws_bytes, void* stream) {
+    if (p->n_seq > 0 && p->n_rows > 0 &&
+        (!q || !k_new || !v_new || !kv || !table || !seq_len || (!decode && !q_start) || !out))
+        return STAR_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(kv, 16) ||
+        !aligned(out, 16))
+        return STAR_ERR_UNSUPPORTED;
+    const AttendPlan pl = plan_attend(*p, decode);
+    star_status st = check_ws(ws, ws_bytes, attend_bytes(pl));
+    if (st != STAR_OK) return st;
+    const int64_t e = p->dtype == STAR_BF16 ? 2 : 4;
+    AttendArgs a = {};
+    a.q = (const char*)q, a.kn = (const char*)k_new, a.vn = (const char*)v_new;
+    a.kv = (char*)kv;
+    a.table = table, a.seq_len = seq_len, a.q_start = decode ? nullptr : q_start;
+    a.out = (char*)out, a.lse = lse;
+    a.part = (char*)ws + STAR_WS_HEADER_BYTES;
+    a.tickets = (uint32_t*)((char*)ws + kHdrTickets);
+    a.err = (int32_t*)((char*)ws + kHdrErrorWord);
+    a.q_stride = p->q_stride * e, a.kv_stride = p->kv_stride * e, a.page_stride = p->page_stride;
+    a.n_seq = p->n_seq, a.n_rows = p->n_rows, a.n_heads = p->n_heads, a.n_kv = p->n_kv_heads;
+    a.g = p->n_heads / p->n_kv_heads;
+    a.ps_log2 = __builtin_ctz(p->page_size), a.n_pages = p->n_pages, a.max_pages = p->max_pages;
+    a.window = p->window, a.sinks = p->sinks;
+    a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
+    const hipError_t err = launch_attend(pl, a, p->dtype, p->head_dim, (hipStream_t)stream);
+    return err == hipSuccess ? STAR_OK : STAR_ERR_HIP;
+}
+
+STAR_API size_t star_attend_decode_workspace_size(const star_attend_params* p) {
+    if (check_attend_params(p) != STAR_OK || p->n_rows != p->n_seq) return 0;
+    return attend_bytes(plan_attend(*p, true));
+}
+
+STAR_API star_status star_attend_decode(const star_attend_params* p, const void* q,
+                                        const void* k_new, const void* v_new, void* kv,
+                                        const int32_t* table, const int32_t* seq_len, void* out,
+                                        float* lse, void* ws, size_t ws_bytes, void* stream) {
+    star_status st = check_attend_params(p);
+    if (st != STAR_OK) return st;
+    if (p->n_rows != p->n_seq) return STAR_ERR_INVALID_ARG;
+    return attend(p, q, k_new, v_new, kv, table, seq_len, nullptr, true, out, lse, ws, ws_bytes,
+                  stream);
+}
+
+STAR_API size_t star_attend_prompt_workspace_size(const star_attend_params* p) {
+    if (check_attend_params(p) != STAR_OK) return 0;
+    return attend_bytes(plan_attend(*p, false));
+}
+
+STAR_API star_status star_attend_prompt(const star_attend_params* p, const void* q,
+                                        const void* k_new, const void* v_new, void* kv,
+                                        const int32_t* table, const int32_t* seq_len,
+                                        const int32_t* q_start, void* out, float* lse, void* ws,
+                                        size_t ws_bytes, void* stream) {
+    star_status st = check_attend_params(p);
+    if (st != STAR_OK) return st;
+    return attend(p, q, k_new, v_new, kv, table, seq_len, q_start, false, out, lse, ws, ws_bytes,
+                  stream);
+}
+
+// ---------------------------------------------------------------------------
 // housekeeping
 // ---------------------------------------------------------------------------
 STAR_API star_status star_workspace_init(void* ws, size_t ws_bytes, void* stream) {

@@ -155,6 +155,47 @@ hipError_t launch_plan(const star_plan_params& p, const PlanPlan& pl, const int3
                        star_move* moves, int32_t* n_moves, char* ws, int32_t* err,
                        hipStream_t stream);
 
+// Pages of the cache (pages.hip): offsets in the workspace.
+constexpr size_t kSlotPlanBytes = 32;
+struct PagesPlan {
+    size_t n_copies_off = 0, copies_off = 0, list_off = 0, slots_off = 0, total = 0;
+};
+PagesPlan plan_pages(const star_pages_params& p);
+hipError_t launch_assign(const star_pages_params& p, const PagesPlan& pl, const int32_t* parent,
+                         const int32_t* new_len, const int32_t* inst_of, const int32_t* table,
+                         const int32_t* seq_len, const int32_t* seq_inst, const int32_t* refs,
+                         void* kv, int32_t* table_out, int32_t* len_out, int32_t* inst_out,
+                         int32_t* refs_out, char* ws, hipStream_t stream);
+hipError_t launch_compact(const star_pages_params& p, const PagesPlan& pl, const int32_t* table,
+                          const int32_t* seq_len, const int32_t* refs, void* kv,
+                          int32_t* table_out, int32_t* refs_out, int32_t* n_live, char* ws,
+                          hipStream_t stream);
+
+// Attention over the cache (attend.hip).
+struct AttendArgs {
+    const char *q, *kn, *vn;    // kn, vn: the new tokens' keys and values
+    char* kv;
+    const int32_t *table, *seq_len, *q_start;   // q_start: null in decode calls
+    char* out;
+    float* lse;
+    char* part;                 // parts of blocks cut between workgroups
+    uint32_t* tickets;          // their arrival counters (workspace header)
+    int32_t* err;
+    int64_t q_stride, kv_stride, page_stride;   // bytes
+    int n_seq, n_rows, n_heads, n_kv, g;        // g: query heads per key-value head
+    int ps_log2, n_pages, max_pages, window, sinks;
+    float scale_log2;           // scale * log2(e)
+    int min_steps;
+};
+struct AttendPlan {
+    int grid = 0;               // workgroups of the row-block kernel
+    int min_steps = 1;          // steps that a workgroup takes at least
+    size_t part_bytes = 0;
+};
+AttendPlan plan_attend(const star_attend_params& p, bool decode);
+hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype, int head_dim,
+                         hipStream_t stream);
+
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t stream);
 
 }  // namespace star

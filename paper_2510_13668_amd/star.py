@@ -26,6 +26,7 @@ STAR_MAX_TOP_K = 1024
 F32, BF16 = 0, 1
 ACT_RELU, ACT_GELU = 0, 1
 DEV_BAD_INST, DEV_BAD_CUR, DEV_BAD_REM = 1, 2, 4
+DEV_BAD_LEN, DEV_BAD_PAGE, DEV_BAD_PARENT, DEV_NO_PAGES = 8, 16, 32, 64
 
 _i32 = ctypes.c_int32
 _P = ctypes.c_void_p
@@ -55,6 +56,20 @@ class PlanParams(ctypes.Structure):
     _fields_ = [("load", LoadParams), ("max_moves", _i32), ("theta_num", _i32),
                 ("theta_den", _i32), ("u_rule", _i32), ("mem_rule", _i32), ("min_rem", _i32),
                 ("mem_cap", ctypes.c_int64)]
+
+
+class PagesParams(ctypes.Structure):
+    _fields_ = [("n_seq", _i32), ("max_pages", _i32), ("n_pages", _i32), ("n_inst", _i32),
+                ("page_size", _i32), ("n_layers", _i32), ("page_bytes", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
+
+
+class AttendParams(ctypes.Structure):
+    _fields_ = [("n_seq", _i32), ("n_rows", _i32), ("n_heads", _i32), ("n_kv_heads", _i32),
+                ("head_dim", _i32), ("dtype", _i32), ("page_size", _i32), ("n_pages", _i32),
+                ("max_pages", _i32), ("window", _i32), ("sinks", _i32), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("kv_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64)]
 
 
 class StarError(RuntimeError):
@@ -124,6 +139,17 @@ def lib():
         L.star_predict_mlp4.restype = ctypes.c_int
         L.star_predict_mlp4.argtypes = ([ctypes.POINTER(Mlp4Params)] + [_P] * 12 +
                                         [ctypes.c_size_t, _P])
+        for fn, params, n_ptrs in (("star_assign_pages", PagesParams, 12),
+                                   ("star_compact_pages", PagesParams, 7),
+                                   ("star_attend_decode", AttendParams, 8),
+                                   ("star_attend_prompt", AttendParams, 9)):
+            size = getattr(L, fn + "_workspace_size")
+            size.restype = ctypes.c_size_t
+            size.argtypes = [ctypes.POINTER(params)]
+            call = getattr(L, fn)
+            call.restype = ctypes.c_int
+            call.argtypes = ([ctypes.POINTER(params)] + [_P] * n_ptrs +
+                             [_P, ctypes.c_size_t, _P])
         L.star_workspace_init.restype = ctypes.c_int
         L.star_workspace_init.argtypes = [_P, ctypes.c_size_t, _P]
         L.star_read_device_error.restype = ctypes.c_int
@@ -369,3 +395,120 @@ def predict_mlp4(p: Mlp4Params, hidden, w1, b1, w2, b2, w3, b3, w4, ema_state, e
                                 rem_len),
         ws.ptr,
         ws.nbytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# pages of the key-value cache
+# ---------------------------------------------------------------------------
+def pages_params(n_seq, max_pages, n_pages, page_size, n_layers, page_bytes, n_inst=1,
+                 page_stride=None, layer_stride=None) -> PagesParams:
+    """Strides in bytes; by default the pool is dense, [n_layers, n_pages, page_bytes]."""
+    if page_stride is None:
+        page_stride = page_bytes
+    if layer_stride is None:
+        layer_stride = n_pages * page_stride
+    return PagesParams(n_seq, max_pages, n_pages, n_inst, page_size, n_layers, page_bytes,
+                       page_stride, layer_stride)
+
+
+def assign_pages_workspace_size(p: PagesParams) -> int:
+    return int(lib().star_assign_pages_workspace_size(ctypes.byref(p)))
+
+
+def assign_pages(p: PagesParams, parent, new_len, inst_of, table, seq_len, seq_inst, refs, kv,
+                 table_out, seq_len_out, seq_inst_out, refs_out, ws: Workspace, stream=None):
+    """star_assign_pages: every slot's pages for its next length, parent and
+    instance.  parent, inst_of: None for none; seq_inst, seq_inst_out may be
+    None where p.n_inst is 1.  Outputs may be their inputs (table_out only
+    without parents)."""
+    _check("star_assign_pages", lib().star_assign_pages(
+        ctypes.byref(p), *_ptrs(parent, new_len, inst_of, table, seq_len, seq_inst, refs,
+                                kv, table_out, seq_len_out, seq_inst_out, refs_out),
+        ws.ptr, ws.nbytes, _stream(stream)))
+
+
+def compact_pages_workspace_size(p: PagesParams) -> int:
+    return int(lib().star_compact_pages_workspace_size(ctypes.byref(p)))
+
+
+def compact_pages(p: PagesParams, table, seq_len, refs, kv, table_out, refs_out, n_live,
+                  ws: Workspace, stream=None):
+    """star_compact_pages: every instance's live pages to its lowest indices."""
+    _check("star_compact_pages", lib().star_compact_pages(
+        ctypes.byref(p), *_ptrs(table, seq_len, refs, kv, table_out, refs_out, n_live),
+        ws.ptr, ws.nbytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# attention over the cache
+# ---------------------------------------------------------------------------
+def attend_params(n_seq, n_rows, n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages,
+                  max_pages, scale, window=0, sinks=0, q_stride=None, kv_stride=None,
+                  page_stride=None) -> AttendParams:
+    """Row strides in elements, the page stride in bytes; dense by default."""
+    if q_stride is None:
+        q_stride = n_heads * head_dim
+    if kv_stride is None:
+        kv_stride = n_kv_heads * head_dim
+    if page_stride is None:
+        page_stride = 2 * n_kv_heads * page_size * head_dim * (2 if dtype == BF16 else 4)
+    return AttendParams(n_seq, n_rows, n_heads, n_kv_heads, head_dim, dtype, page_size, n_pages,
+                        max_pages, window, sinks, float(scale), q_stride, kv_stride, page_stride)
+
+
+_TORCH_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _strided(t: torch.Tensor, dtype, shape, stride: int) -> int:
+    """The address of a tensor of `shape` that is dense but for its first
+    dimension, whose steps are `stride` elements."""
+    if not t.is_cuda:
+        raise ValueError("libstar takes device tensors")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    got, dense = t.stride(), 1
+    for n, step in zip(reversed(shape[1:]), reversed(got[1:])):
+        if step != dense and n > 1:
+            raise ValueError("only the first dimension may have a stride of its own")
+        dense *= n
+    if shape[0] > 1 and got[0] != stride:
+        raise ValueError(f"a first stride of {got[0]}, the parameters say {stride}")
+    return t.data_ptr()
+
+
+def _attend_ptrs(p: AttendParams, q, k_new, v_new, kv):
+    dt, D = _TORCH_DTYPES[p.dtype], p.head_dim
+    new = (p.n_rows, p.n_kv_heads, D)
+    return (_strided(q, dt, (p.n_rows, p.n_heads, D), p.q_stride),
+            _strided(k_new, dt, new, p.kv_stride), _strided(v_new, dt, new, p.kv_stride),
+            _strided(kv, dt, (p.n_pages, 2, p.n_kv_heads, p.page_size, D),
+                     p.page_stride // dt.itemsize))
+
+
+def attend_decode_workspace_size(p: AttendParams) -> int:
+    return int(lib().star_attend_decode_workspace_size(ctypes.byref(p)))
+
+
+def attend_decode(p: AttendParams, q, k_new, v_new, kv, table, seq_len, out, lse, ws: Workspace,
+                  stream=None):
+    """star_attend_decode: one new token a slot.  q, k_new, v_new: [n_seq,
+    heads, head_dim], rows p.q_stride and p.kv_stride elements apart (columns
+    of one projection's output do); kv: one layer of the pool, [n_pages, 2,
+    n_kv_heads, page_size, head_dim]; lse: None for none."""
+    _check("star_attend_decode", lib().star_attend_decode(
+        ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
+        *_ptrs(table, seq_len, out, lse), ws.ptr, ws.nbytes, _stream(stream)))
+
+
+def attend_prompt_workspace_size(p: AttendParams) -> int:
+    return int(lib().star_attend_prompt_workspace_size(ctypes.byref(p)))
+
+
+def attend_prompt(p: AttendParams, q, k_new, v_new, kv, table, seq_len, q_start, out, lse,
+                  ws: Workspace, stream=None):
+    """star_attend_prompt: several new tokens a slot, rows q_start[b] ..
+    q_start[b + 1] - 1 of q, k_new, v_new, out and lse; otherwise as
+    attend_decode."""
+    _check("star_attend_prompt", lib().star_attend_prompt(
+        ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
+        *_ptrs(table, seq_len, q_start, out, lse), ws.ptr, ws.nbytes, _stream(stream)))
