@@ -1,6 +1,7 @@
 // Attention over the paged key-value cache (include/star.h, "attention over
 // the cache"): the row-block kernel behind star_attend_decode and short
 // star_attend_prompt calls, and the kernel that stores a prompt's new tokens.
+#include "attend.hpp"
 #include "star_common.hpp"
 #include "star_internal.hpp"
 
@@ -8,12 +9,10 @@ namespace star {
 
 namespace {
 
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kRows = 16;        // query rows of one block (an MFMA's columns)
+constexpr int kRows = kBlockRows;
 constexpr int kThreads = 256;    // four waves share a block's keys
 constexpr int kWaves = kThreads / kWave;
-constexpr float kLn2 = 0.69314718055994531f;
+static_assert(kWaves == kBlockWaves, "one tile a wave and step");
 
 template <int kDtype> struct Elem;
 template <> struct Elem<STAR_BF16> {
@@ -22,59 +21,6 @@ template <> struct Elem<STAR_BF16> {
 template <> struct Elem<STAR_F32> {
     static constexpr int kBytes = 4, kTile = 16;
 };
-
-// The keys that the rows at positions p0..p1 of one request can see, in tiles:
-// nA tiles of first tokens (sinks), then tiles b0.. up to p1's.
-struct Tiles {
-    int nA, b0, n;
-    __device__ int at(int u) const { return u < nA ? u : u - nA + b0; }
-};
-template <int kTile>
-__device__ inline Tiles tiles_of(const AttendArgs& a, int p0, int p1) {
-    Tiles t;
-    const int lo = a.window && p0 >= a.window ? p0 - a.window + 1 : 0;
-    t.b0 = lo / kTile;
-    const int s = a.window ? (a.sinks < p1 + 1 ? a.sinks : p1 + 1) : 0;
-    const int nA = (s + kTile - 1) / kTile;
-    t.nA = nA < t.b0 ? nA : t.b0;
-    t.n = p1 < 0 ? 0 : t.nA + p1 / kTile - t.b0 + 1;
-    return t;
-}
-
-// One request of the call: L cached tokens, the last T of them new, its rows
-// of q from row0 on.  A request that breaks a precondition has no rows.
-struct Slot {
-    int L, T, row0, blocks;   // blocks of kRows rows
-    int steps;                // scheduling steps of one block (kWaves tiles each)
-};
-template <int kTile>
-__device__ inline Slot slot_of(const AttendArgs& a, int b, int32_t& bad) {
-    Slot s;
-    s.L = a.seq_len[b];
-    bool ok = s.L >= 0 && s.L <= a.max_pages << a.ps_log2;
-    if (a.q_start) {
-        const int from = a.q_start[b], to = a.q_start[b + 1];
-        s.row0 = from;
-        s.T = to - from;
-        ok = ok && from >= 0 && to >= from && to <= a.n_rows && s.T <= s.L;
-    } else {
-        s.row0 = b;
-        s.T = 1;                       // an empty request's row is all zeros
-    }
-    if (!ok) {
-        bad |= STAR_DEV_BAD_LEN;
-        s.L = s.T = 0;
-    }
-    s.blocks = (int)(((int64_t)s.T * a.g + kRows - 1) / kRows);
-    int n = tiles_of<kTile>(a, s.L - 1, s.L - 1).n;
-    if (s.T > 1 && a.window) {          // a block's rows span at most kRows positions
-        const int all = (s.L - 1) / kTile + 1;
-        n = n + (kRows + kTile - 1) / kTile + 1;
-        n = n < all ? n : all;
-    }
-    s.steps = n > kWaves ? (n + kWaves - 1) / kWaves : 1;
-    return s;
-}
 
 // maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48: two register
 // swaps between rows of 16 lanes instead of LDS permutes
@@ -145,13 +91,6 @@ __device__ inline void load_k(const char* row, int c, u32x4* to) {
         to[i] = *(const u32x4*)(row + i * 64 + c * 16);
 }
 
-// A product's result may be read a number of wait states after it is issued (11
-// for these shapes).  The compiler counts them within a basic block; where a
-// branch came between, it was seen to count the longer of two paths only
-// (fp32, 256 wide: the last product was missing from one register in four).
-// So results meet 16 wait states before any branch.
-__device__ inline void settle(f32x4& x) { asm volatile("s_nop 15" : "+v"(x)); }
-
 // S^T += K Q^T for one 16-token half
 template <int kDtype, int D>
 __device__ inline f32x4 scores(const u32x4* k, const u32x4* q) {
@@ -212,30 +151,6 @@ __device__ inline void accumulate(const uint32_t (&v)[Tile<kDtype, D>::kRowsV]
     settle(o[D / 16 - 1]);          // the last one issued
 }
 
-template <int kDtype>
-__device__ inline bool not_finite(uint32_t w) {
-    if constexpr (kDtype == STAR_F32)
-        return (w & 0x7F800000u) == 0x7F800000u;
-    else
-        return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
-}
-
-// the larger magnitudes, value by value (and the signs dropped)
-template <int kDtype>
-__device__ inline uint32_t larger(uint32_t a, uint32_t w) {
-    if constexpr (kDtype == STAR_F32) return max(a, w & 0x7FFFFFFFu);
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
-                                            __builtin_bit_cast(u16x2, a),
-                                            __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
-}
-// the word with its values that are not finite at 0
-template <int kDtype>
-__device__ inline uint32_t finite_part(uint32_t w) {
-    if constexpr (kDtype == STAR_F32) return not_finite<kDtype>(w) ? 0u : w;
-    const uint32_t lo = (w & 0x7F80u) == 0x7F80u ? 0u : w & 0xFFFFu;
-    const uint32_t hi = (w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u;
-    return lo | hi;
-}
 template <int kDtype>
 __device__ inline float value_at(const uint32_t* w, int i) {
     if constexpr (kDtype == STAR_F32) return __uint_as_float(w[i]);
@@ -661,7 +576,9 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     static_assert(512 <= kMaxTickets, "one ticket per workgroup");
     pl.min_steps = 2;
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
-    (void)decode;
+    const int64_t rows = (int64_t)p.n_rows * (p.n_heads / p.n_kv_heads);
+    pl.tiled = !decode && p.dtype == STAR_BF16 && p.head_dim <= 128 &&
+               rows >= 64 * (int64_t)p.n_seq;
     return pl;
 }
 
@@ -679,6 +596,7 @@ hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype
         if (e1 != hipSuccess) return e1;
         a.kn = a.vn = nullptr;
     }
+    if (pl.tiled) return launch_attend_tiles(a, head_dim, stream);
     if (dtype == STAR_BF16) {
         if (head_dim == 64) return launch_rows<STAR_BF16, 64>(a, pl.grid, stream);
         if (head_dim == 128) return launch_rows<STAR_BF16, 128>(a, pl.grid, stream);

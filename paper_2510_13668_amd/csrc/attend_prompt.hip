@@ -1,0 +1,388 @@
+// Attention of many new tokens over the paged key-value cache: the bf16 kernel
+// of star_attend_prompt whose keys and values go through LDS.
+#include <type_traits>
+
+#include "attend.hpp"
+#include "star_common.hpp"
+#include "star_internal.hpp"
+
+namespace star {
+
+namespace {
+
+constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
+constexpr int kBN = 64;          // tokens of a tile, 16 a wave to load
+constexpr int kThreads = 256, kWaves = 4;
+constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may lag
+
+typedef __attribute__((address_space(3))) char* lds_t;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int D>
+struct Lay {
+    static constexpr int kRow = 2 * D;            // bytes of a token's keys (or values)
+    static constexpr int kChunks = kRow / 16;     // 16-byte chunks of a row
+    static constexpr int kTile = kBN * kRow;      // bytes of a tile's keys
+    static constexpr int kRowsPerLoad = 1024 / kRow;
+    static constexpr int kLoads = 16 / kRowsPerLoad;   // 1 KiB loads of 16 tokens
+    // Chunk c of row r lies at chunk c ^ f(r) of the row.  Keys: 16 lanes read
+    // one chunk of 16 rows; values: 32 lanes read 32 bytes of 4 rows and the 32
+    // bytes beside; either way every bank is read once.
+    __device__ static int fk(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+    __device__ static int fv(int r) { return D == 64 ? ((r >> 1) & 1) * 4 : (r & 3) * 4; }
+};
+
+// the maximum of lanes l and l ^ 32
+__device__ inline float pair_max(float v) {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ inline float pair_sum(float v) {
+    auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// ---------------------------------------------------------------------------
+// One workgroup: 128 (token, query head) rows of one request that share a
+// key-value head, tokens before heads, so that a group's heads share every
+// tile.  Lane l of a wave owns row l % 32: S^T [tokens x rows] = K Q^T gives it
+// the scores of half the tokens, its exponentials are in place as the second
+// operand of O^T [d x rows] = V^T P^T, and the softmax needs one exchange with
+// lane l ^ 32 a tile.  V's fragments are read from LDS transposed.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a) {
+    using Y = Lay<D>;
+    constexpr int kSteps = D / 16;       // contraction steps of a score
+    constexpr int kOut = D / 32;         // 32-wide blocks of the output
+    __shared__ __attribute__((aligned(1024))) char s_kv[2][2][Y::kTile];
+    __shared__ int64_t s_tmp[kWaves + 1];
+    __shared__ int s_slot[2], s_fix[2];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int r32 = lane & 31, half = lane >> 5;
+
+    // which request and which of its blocks of rows; the last ones, with the
+    // longest prefixes, first
+    const int head = blockIdx.x % a.n_kv;
+    {
+        const int per = (a.n_seq + kThreads - 1) / kThreads;
+        int64_t mine = 0, total;
+        int32_t bad = 0;
+        auto blocks = [&](int b) {
+            const Slot s = slot_of<kBN>(a, b, bad);
+            return ((int64_t)s.T * a.g + kBM - 1) / kBM;
+        };
+        for (int b = tid * per; b < min(a.n_seq, (tid + 1) * per); ++b) mine += blocks(b);
+        if (blockIdx.x == 0) report_error(a.err, bad);
+        const int64_t before =
+            block_exclusive_scan_i64<kThreads>(mine, OpAdd(), 0, s_tmp, &total);
+        const int64_t at = total - 1 - blockIdx.x / a.n_kv;
+        if (at < 0) return;
+        if (before <= at && at < before + mine) {
+            int64_t base = before;
+            for (int b = tid * per;; ++b) {
+                const int64_t n = blocks(b);
+                if (at < base + n) {
+                    s_slot[0] = b;
+                    s_slot[1] = (int)(at - base);
+                    break;
+                }
+                base += n;
+            }
+        }
+        __syncthreads();
+    }
+    const int b = __builtin_amdgcn_readfirstlane(s_slot[0]);
+    int32_t ignored = 0;
+    const Slot s = slot_of<kBN>(a, b, ignored);
+    const int all_rows = s.T * a.g;                  // (below 2^31 over all requests)
+    const int row_from = __builtin_amdgcn_readfirstlane(s_slot[1]) * kBM;
+    const int first = s.L - s.T;
+    auto pos_of = [&](int row) { return first + min(row, all_rows - 1) / a.g; };
+    const int p0 = pos_of(row_from), p1 = pos_of(row_from + kBM - 1);       // the workgroup's
+    const int wave_row = row_from + 32 * wave;
+    const int w0 = pos_of(wave_row), w1 = pos_of(wave_row + 31);            // the wave's
+    const bool active = wave_row < all_rows;
+    const bool live = wave_row + r32 < all_rows;
+    const int row = min(wave_row + r32, all_rows - 1);
+    const int pos = live ? first + row / a.g : -1;
+    const int64_t q_row = s.row0 + row / a.g;
+    const int q_head = head * a.g + row % a.g;
+
+    // a negative scale turns the queries' signs, so that the largest score is
+    // the largest product
+    const float c = fabsf(a.scale_log2);
+    const uint32_t turn = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    u32x4 q[kSteps];
+    {
+        const char* p = a.q + q_row * a.q_stride + (int64_t)q_head * Y::kRow + half * 16;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            q[i] = live ? *(const u32x4*)(p + 32 * i) : u32x4{0, 0, 0, 0};
+            q[i] ^= turn;
+        }
+    }
+
+    const int32_t* pages = a.table + (int64_t)b * a.max_pages;
+    const Tiles tl = tiles_of<kBN>(a, p0, p1);
+    const int64_t v_off = (int64_t)a.n_kv * Y::kRow << a.ps_log2;
+    const int64_t head_off = (int64_t)head * Y::kRow << a.ps_log2;
+    int32_t err = 0;
+
+    // lane x % 4's sixteen tokens of a tile: their page, or -1 where no row of
+    // the workgroup sees one of them; a bad page reports and reads page 0
+    struct Pages {
+        int page;
+        bool ok;
+    };
+    auto look_up = [&](int u) {
+        const int j = tl.at(u) * kBN + 16 * (lane & 3);
+        const bool seen = j <= p1 && (!a.window || j + 15 > p0 - a.window || j < a.sinks);
+        return seen ? pages[j >> a.ps_log2] : -1;
+    };
+    auto check = [&](int u, int page) {
+        const int j = tl.at(u) * kBN + 16 * (lane & 3);
+        const bool seen = j <= p1 && (!a.window || j + 15 > p0 - a.window || j < a.sinks);
+        Pages x;
+        x.ok = seen && (uint32_t)page < (uint32_t)a.n_pages;
+        if (seen && !x.ok) err |= STAR_DEV_BAD_PAGE;
+        x.page = x.ok ? page : 0;
+        return x;
+    };
+    // this wave's sixteen tokens of a tile: keys and values into registers,
+    // and from there into a buffer once the one before it is done with
+    const int st_row = lane / Y::kChunks, st_ch = lane % Y::kChunks;
+    const int g_off = st_row * Y::kRow + st_ch * 16;
+    u32x4 next_k[Y::kLoads], next_v[Y::kLoads];
+    auto address = [&](int u, const Pages& x) {
+        const int page = __builtin_amdgcn_readlane(x.page, wave);
+        const int in = (tl.at(u) * kBN + 16 * wave) & ((1 << a.ps_log2) - 1);
+        return a.kv + (int64_t)page * a.page_stride + head_off + (int64_t)in * Y::kRow + g_off;
+    };
+    auto load = [&](const char* base, u32x4 (&to)[Y::kLoads]) {
+#pragma unroll
+        for (int i = 0; i < Y::kLoads; ++i) to[i] = *(const u32x4*)(base + 1024 * i);
+    };
+    auto store_k = [&](int to) {
+#pragma unroll
+        for (int i = 0; i < Y::kLoads; ++i) {
+            const int rr = i * Y::kRowsPerLoad + st_row;
+            *(u32x4*)(&s_kv[to][0][0] + (wave * 16 + rr) * Y::kRow + (st_ch ^ Y::fk(rr)) * 16) =
+                next_k[i];
+        }
+    };
+    // values of a tile that not every row sees: those that are not finite
+    // would reach the other rows as 0 times infinity, so they stay out of LDS,
+    // and the tile is marked (by its number, so that no mark needs clearing)
+    auto store_v = [&](int to, int u, bool plain) {
+        if (!plain) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int i = 0; i < Y::kLoads; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) big = larger<STAR_BF16>(big, next_v[i][x]);
+            if (__any(not_finite<STAR_BF16>(big))) {
+#pragma unroll
+                for (int i = 0; i < Y::kLoads; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        next_v[i][x] = finite_part<STAR_BF16>(next_v[i][x]);
+                s_fix[to] = u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < Y::kLoads; ++i) {
+            const int rr = i * Y::kRowsPerLoad + st_row;
+            *(u32x4*)(&s_kv[to][1][0] + (wave * 16 + rr) * Y::kRow + (st_ch ^ Y::fv(rr)) * 16) =
+                next_v[i];
+        }
+    };
+
+    f32x16 o[kOut];
+#pragma unroll
+    for (int i = 0; i < kOut; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[i][x] = 0.0f;
+    float m = -INFINITY, l = 0.0f;      // l: this lane's tokens only
+
+    // lane addresses of the fragments in a tile
+    const int k_base = r32 * Y::kRow, k_x = (half ^ Y::fk(r32)) * 16;
+    const int i16 = lane & 15;
+    const int v_base = (4 * half + (i16 >> 2)) * Y::kRow + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
+    const int v_x = Y::fv(i16 >> 2) * 16;
+    // (fv depends on a row's two lowest bits, D == 64: on its second; the
+    // fragments' first rows are multiples of four)
+
+    // whether all tokens of a tile are visible to all rows from p to p_last
+    auto plain_to = [&](int u, uint32_t ok4, int p, int p_last) {
+        const int j0 = tl.at(u) * kBN;
+        return ok4 == 15u && j0 + kBN - 1 <= p &&
+               (!a.window || j0 > p_last - a.window || j0 + kBN <= a.sinks);
+    };
+
+    Pages now = check(0, look_up(0));
+    uint32_t ok4 = (uint32_t)__ballot(now.ok) & 15u;
+    if (tid < 2) s_fix[tid] = -1;
+    __syncthreads();
+    {
+        const char* from = address(0, now);
+        load(from, next_k);
+        load(from + v_off, next_v);
+        store_k(0);
+        store_v(0, 0, plain_to(0, ok4, p0, p1));
+    }
+    int page_next = look_up(min(1, tl.n - 1));
+    for (int u = 0; u < tl.n; ++u) {
+        __syncthreads();          // tile u is in its buffer, and the other one is done with
+        const lds_t kb = (lds_t)&s_kv[u & 1][0][0], vb = (lds_t)&s_kv[u & 1][1][0];
+        const int j0 = tl.at(u) * kBN;
+        // (the last tile is loaded twice, so that no step hangs on a condition)
+        const int un = min(u + 1, tl.n - 1);
+        const Pages here = now;
+        const uint32_t ok_here = ok4;
+        now = check(un, page_next);
+        ok4 = (uint32_t)__ballot(now.ok) & 15u;
+        const char* from = address(un, now);
+        load(from, next_k);
+        page_next = look_up(min(u + 2, tl.n - 1));
+
+        f32x16 z[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) z[t][x] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const bf16x8_t kf = *(__attribute__((address_space(3))) const bf16x8_t*)(
+                    kb + t * 32 * Y::kRow + k_base + ((32 * i) ^ k_x));
+                z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    kf, __builtin_bit_cast(bf16x8_t, q[i]), z[t], 0, 0, 0);
+            }
+        }
+        load(from + v_off, next_v);
+        auto sees = [&](int j) {
+            return ((ok_here >> ((j - j0) >> 4)) & 1) && j <= pos &&
+                   (!a.window || j > pos - a.window || j < a.sinks);
+        };
+        settle(z[0]);
+        settle(z[1]);
+        if (!plain_to(u, ok_here, w0, w1)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    if (!sees(j0 + 32 * t + 8 * (x / 4) + 4 * half + x % 4)) z[t][x] = -INFINITY;
+        }
+
+        float top = z[0][0];
+#pragma unroll
+        for (int x = 1; x < 16; ++x) top = fmaxf(top, z[0][x]);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) top = fmaxf(top, z[1][x]);
+        top = pair_max(top) * c;
+        // the reference may lag the maximum by 2^kLazy: the sums have the room
+        // (fp32), and bf16's relative step is the same everywhere
+        if (__any(top > m + kLazy)) {
+            const float peak = fmaxf(m, top);
+            const float f = __builtin_amdgcn_exp2f(m - (peak == -INFINITY ? 0.0f : peak));
+            m = peak;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) o[i] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;      // nothing seen yet: all p are 0
+        u32x4 p[4];                // 16 tokens each, as the second product takes them
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x], c, -ref));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x + 1], c, -ref));
+                l += e0;
+                l += e1;
+                p[2 * t + x / 8][(x % 8) / 2] = pack_bf16x2_rne(e0, e1);
+            }
+        store_k((u + 1) & 1);
+#pragma unroll
+        for (int s4 = 0; s4 < 4; ++s4)
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) {
+                const lds_t at = vb + v_base + s4 * 16 * Y::kRow + ((64 * i) ^ v_x);
+                typedef __attribute__((address_space(3))) s16x4* tr_t;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 8 * Y::kRow));
+                const u32x2 x0 = __builtin_bit_cast(u32x2, lo), x1 = __builtin_bit_cast(u32x2, hi);
+                const u32x4 va = {x0[0], x0[1], x1[0], x1[1]};
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, p[s4]), o[i], 0,
+                    0, 0);
+            }
+        if (s_fix[u & 1] == u) {
+            // the values that were kept out reach the rows that see them (their
+            // probabilities are positive), from the cache
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) settle(o[i]);
+            for (int j = 0; j < kBN; ++j) {
+                const int page = __builtin_amdgcn_readlane(here.page, j >> 4);
+                const char* raw = a.kv + (int64_t)page * a.page_stride + head_off + v_off +
+                                  (int64_t)((j0 + j) & ((1 << a.ps_log2) - 1)) * Y::kRow + half * 8;
+                if (!sees(j0 + j)) continue;
+#pragma unroll
+                for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const u32x2 w = *(const u32x2*)(raw + i * 64 + x * 16);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const float v = __uint_as_float(y & 1 ? w[y / 2] & 0xFFFF0000u
+                                                                  : w[y / 2] << 16);
+                            if (!(fabsf(v) < INFINITY)) o[i][4 * x + y] += v;
+                        }
+                    }
+            }
+        }
+        store_v((u + 1) & 1, un == u ? -2 : un, plain_to(un, ok4, p0, p1));
+    }
+#pragma unroll
+    for (int i = 0; i < kOut; ++i) settle(o[i]);
+    if (err && lane < 4) report_error(a.err, err);
+
+    l = pair_sum(l);
+    if (!live) return;
+    const int64_t at = q_row * a.n_heads + q_head;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // a row that sees nothing is 0
+    char* to = a.out + at * Y::kRow + half * 8;
+#pragma unroll
+    for (int i = 0; i < kOut; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; x += 4) {
+            u32x2 w;
+            w[0] = pack_bf16x2_rne(o[i][x] * inv, o[i][x + 1] * inv);
+            w[1] = pack_bf16x2_rne(o[i][x + 2] * inv, o[i][x + 3] * inv);
+            *(u32x2*)(to + i * 64 + x * 4) = w;
+        }
+    if (a.lse && half == 0)
+        a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int D>
+hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
+    // blocks of rows: every request has one that is not full at most
+    const int64_t blocks = (int64_t)a.n_rows * a.g / kBM + a.n_seq;
+    const int64_t grid = blocks * a.n_kv;
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attend_tiles_kernel<D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
+                       a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream) {
+    if (head_dim == 64) return launch_tiles<64>(a, stream);
+    return launch_tiles<128>(a, stream);
+}
+
+}  // namespace star

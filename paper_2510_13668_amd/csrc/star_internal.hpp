@@ -191,10 +191,13 @@ struct AttendPlan {
     int grid = 0;               // workgroups of the row-block kernel
     int min_steps = 1;          // steps that a workgroup takes at least
     size_t part_bytes = 0;
+    bool tiled = false;         // the kernel of attend_prompt.hip
 };
 AttendPlan plan_attend(const star_attend_params& p, bool decode);
 hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype, int head_dim,
                          hipStream_t stream);
+
+hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream);
 
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t stream);
 
