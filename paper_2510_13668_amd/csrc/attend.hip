@@ -1,6 +1,6 @@
 // Attention over the paged key-value cache (include/star.h, "attention over
 // the cache"): the row-block kernel behind star_attend_decode and short
-// star_attend_prompt calls, and the kernel that stores a prompt's new tokens.
+// star_attend_prompt calls.
 #include "attend.hpp"
 #include "star_common.hpp"
 #include "star_internal.hpp"
@@ -255,8 +255,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
 
         const Tiles tl = tiles_of<kT>(a, p0, s.L > 0 ? p1 : -1);
         const int32_t* pages = a.table + (int64_t)b * a.max_pages;
-        const char* kn = a.kn ? a.kn + (int64_t)b * a.kv_stride + (int64_t)head * D * kB : nullptr;
-        const char* vn = a.kn ? a.vn + (int64_t)b * a.kv_stride + (int64_t)head * D * kB : nullptr;
+        // the new tokens come from their own arrays (row 0: position `first`):
+        // the cache is written beside, and no one reads them there
+        const char* kn = a.kn + (int64_t)s.row0 * a.kv_stride + (int64_t)head * D * kB;
+        const char* vn = a.vn + (int64_t)s.row0 * a.kv_stride + (int64_t)head * D * kB;
         const int64_t v_off = (int64_t)a.n_kv * D * kB << a.ps_log2;   // values after keys
 
         // where half h of tile t lies; a half that no row of the block sees is
@@ -281,15 +283,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
                 hf[h] = half_at(t, h);
                 const char* kb = hf[h].base + r * (D * kB);
                 const char* vb = hf[h].base + v_off + c * 4 * (D * kB) + r * TT::kRowV;
-                // the call's new token comes from its own arrays: the cache is
-                // written beside, and no one reads it there
-                const int at = a.kn ? s.L - 1 - (t * kT + h * 16) : -1;
-                if ((uint32_t)at < 16u) {
-                    load_k<kDtype, D>(r == at ? kn : kb, c, f.k[h]);
+                const int j = t * kT + h * 16;
+                if (j + 16 > first && s.L > 0) {
+                    auto row_at = [&](const char* rows, int token, const char* cached) {
+                        return token < first ? cached
+                                             : rows + (int64_t)(min(token, s.L - 1) - first) *
+                                                          a.kv_stride;
+                    };
+                    load_k<kDtype, D>(row_at(kn, j + r, kb), c, f.k[h]);
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        load_row<kDtype, D>(4 * c + x == at ? vn + r * TT::kRowV
-                                                            : vb + x * (D * kB),
+                        load_row<kDtype, D>(row_at(vn + r * TT::kRowV, j + 4 * c + x,
+                                                   vb + x * (D * kB)),
                                             f.v[4 * h + x]);
                 } else {
                     load_k<kDtype, D>(kb, c, f.k[h]);
@@ -412,21 +417,21 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
             }
         }
 
-        // the new token joins the cache, once per key-value head: by the wave
-        // of the block's last tile, where that tile is in this piece
-        if (a.kn && s.L > 0 && row_from == 0) {
-            const int last = tl.n - 1;
-            if (last % kWaves == wave && last / kWaves >= step0 && last / kWaves < step0 + steps) {
-                const int j = s.L - 1;
-                const int page = __builtin_amdgcn_readfirstlane(pages[j >> a.ps_log2]);
-                if ((uint32_t)page < (uint32_t)a.n_pages && lane < D * kB / 16) {
-                    char* to = a.kv + (int64_t)page * a.page_stride +
-                               (((int64_t)head << a.ps_log2) + (j & ((1 << a.ps_log2) - 1))) *
-                                   (D * kB) +
-                               lane * 16;
-                    *(u32x4*)to = *(const u32x4*)(kn + lane * 16);
-                    *(u32x4*)(to + v_off) = *(const u32x4*)(vn + lane * 16);
-                }
+        // new tokens join the cache with the block that holds their first row,
+        // once per key-value head
+        if (step0 == 0 && s.L > 0) {
+            const int i0 = (row_from + a.g - 1) / a.g, i1 = (row_from + rows - 1) / a.g;
+            constexpr int kPer = D * kB / 16;             // 16-byte pieces of a row
+            for (int x = tid; x < (i1 - i0 + 1) * 2 * kPer; x += kThreads) {
+                const int i = i0 + x / (2 * kPer), d = x % kPer * 16, j = first + i;
+                const bool value = x / kPer & 1;
+                const int page = pages[j >> a.ps_log2];
+                if ((uint32_t)page < (uint32_t)a.n_pages)
+                    *(u32x4*)(a.kv + (int64_t)page * a.page_stride + (value ? v_off : 0) +
+                              (((int64_t)head << a.ps_log2) + (j & ((1 << a.ps_log2) - 1))) *
+                                  (D * kB) +
+                              d) =
+                        *(const u32x4*)((value ? vn : kn) + (int64_t)i * a.kv_stride + d);
             }
         }
 
@@ -525,42 +530,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
     if (err && lane == 0) report_error(a.err, err);
 }
 
-// ---------------------------------------------------------------------------
-// The new tokens of prompts into their pages: one workgroup per token, 16
-// bytes a thread.
-// ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes) {
-    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
-        // the request whose rows hold this one: the last that starts at or before it
-        int lo = 0, hi = a.n_seq;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (a.q_start[mid] <= row) lo = mid + 1;
-            else hi = mid;
-        }
-        const int b = lo - 1;
-        if (b < 0) continue;
-        const int from = a.q_start[b], to = a.q_start[b + 1], L = a.seq_len[b];
-        if (from < 0 || row >= to || to > a.n_rows || L < 0 || L > a.max_pages << a.ps_log2 ||
-            to - from > L)
-            continue;
-        const int j = (int)(L - (to - from) + (row - from));
-        const int page = a.table[(int64_t)b * a.max_pages + (j >> a.ps_log2)];
-        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-        const int in = j & ((1 << a.ps_log2) - 1);
-        const int all = a.n_kv * row_bytes;               // bytes of one token's keys
-        char* base = a.kv + (int64_t)page * a.page_stride;
-        for (int x = threadIdx.x * 16; x < 2 * all; x += kThreads * 16) {
-            const int y = x < all ? x : x - all;
-            const int head = y / row_bytes, d = y - head * row_bytes;
-            const char* src = (x < all ? a.kn : a.vn) + row * a.kv_stride + y;
-            char* dst = base + ((int64_t)((x < all ? 0 : a.n_kv) + head) << a.ps_log2) * row_bytes +
-                        (int64_t)in * row_bytes + d;
-            *(u32x4*)dst = *(const u32x4*)src;
-        }
-    }
-}
-
 template <int kDtype, int D>
 hipError_t launch_rows(const AttendArgs& a, int grid, hipStream_t stream) {
     hipLaunchKernelGGL((attend_rows_kernel<kDtype, D>), dim3(grid), dim3(kThreads), 0, stream, a);
@@ -587,15 +556,6 @@ hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype
     AttendArgs a = args;
     a.min_steps = pl.min_steps;
     if (a.n_seq == 0 || a.n_rows == 0) return hipSuccess;
-    if (a.q_start && a.kn) {
-        const int e = dtype == STAR_BF16 ? 2 : 4;
-        const int grid = a.n_rows < 4096 ? a.n_rows : 4096;
-        hipLaunchKernelGGL(store_tokens_kernel, dim3(grid), dim3(kThreads), 0, stream, a,
-                           head_dim * e);
-        hipError_t e1 = hipGetLastError();
-        if (e1 != hipSuccess) return e1;
-        a.kn = a.vn = nullptr;
-    }
     if (pl.tiled) return launch_attend_tiles(a, head_dim, stream);
     if (dtype == STAR_BF16) {
         if (head_dim == 64) return launch_rows<STAR_BF16, 64>(a, pl.grid, stream);

@@ -63,29 +63,57 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int r32 = lane & 31, half = lane >> 5;
 
-    // which request and which of its blocks of rows; the last ones, with the
-    // longest prefixes, first
-    const int head = blockIdx.x % a.n_kv;
-    {
+    // which request and which of its blocks of rows: those with the longest
+    // prefixes first, so that the launch ends on short ones
+    const int head = blockIdx.x % a.n_kv, nth = blockIdx.x / a.n_kv;
+    int b, block;
+    if (a.n_seq <= 64) {
+        // one request a lane, every wave by itself: the largest last position X
+        // that more than nth blocks reach, then the blocks at X in order
+        int32_t bad = 0;
+        Slot s = {0, 0, 0, 0, 0};
+        if (lane < a.n_seq) s = slot_of<kBN>(a, lane, bad);
+        if (blockIdx.x == 0 && wave == 0) report_error(a.err, bad);
+        const int n = (s.T * a.g + kBM - 1) / kBM;
+        // the request's blocks whose last position is X or more
+        auto reach = [&](int x) {
+            const int t = x - (s.L - s.T);
+            return t <= 0 ? n : t >= s.T ? 0 : n - (t * a.g >> 7);
+        };
+        static_assert(kBM == 128, "reach divides by it");
+        auto all = [&](int mine) {
+            return __builtin_amdgcn_readlane(wave_incl_add_i32(mine), 63);
+        };
+        if (nth >= all(n)) return;
+        int lo = 0, hi = 64;
+        while (__any(hi < s.L)) hi <<= 1;                // (L is at most 2^30)
+        while (hi - lo > 1) {
+            const int mid = lo + (hi - lo) / 2;
+            if (all(reach(mid)) > nth) lo = mid;
+            else hi = mid;
+        }
+        const int rank = nth - all(reach(lo + 1)), here = reach(lo) - reach(lo + 1);
+        const int upto = wave_incl_add_i32(here);
+        const uint64_t past = __ballot(upto > rank);
+        b = __builtin_ctzll(past);
+        block = __builtin_amdgcn_readlane(n - reach(lo) + rank - (upto - here), b);
+    } else {
         const int per = (a.n_seq + kThreads - 1) / kThreads;
         int64_t mine = 0, total;
         int32_t bad = 0;
-        auto blocks = [&](int b) {
-            const Slot s = slot_of<kBN>(a, b, bad);
-            return ((int64_t)s.T * a.g + kBM - 1) / kBM;
-        };
-        for (int b = tid * per; b < min(a.n_seq, (tid + 1) * per); ++b) mine += blocks(b);
+        auto blocks = [&](int x) { return (slot_of<kBN>(a, x, bad).T * a.g + kBM - 1) / kBM; };
+        for (int x = tid * per; x < min(a.n_seq, (tid + 1) * per); ++x) mine += blocks(x);
         if (blockIdx.x == 0) report_error(a.err, bad);
         const int64_t before =
             block_exclusive_scan_i64<kThreads>(mine, OpAdd(), 0, s_tmp, &total);
-        const int64_t at = total - 1 - blockIdx.x / a.n_kv;
+        const int64_t at = total - 1 - nth;
         if (at < 0) return;
         if (before <= at && at < before + mine) {
             int64_t base = before;
-            for (int b = tid * per;; ++b) {
-                const int64_t n = blocks(b);
+            for (int x = tid * per;; ++x) {
+                const int n = blocks(x);
                 if (at < base + n) {
-                    s_slot[0] = b;
+                    s_slot[0] = x;
                     s_slot[1] = (int)(at - base);
                     break;
                 }
@@ -93,12 +121,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             }
         }
         __syncthreads();
+        b = __builtin_amdgcn_readfirstlane(s_slot[0]);
+        block = __builtin_amdgcn_readfirstlane(s_slot[1]);
     }
-    const int b = __builtin_amdgcn_readfirstlane(s_slot[0]);
     int32_t ignored = 0;
     const Slot s = slot_of<kBN>(a, b, ignored);
     const int all_rows = s.T * a.g;                  // (below 2^31 over all requests)
-    const int row_from = __builtin_amdgcn_readfirstlane(s_slot[1]) * kBM;
+    const int row_from = block * kBM;
     const int first = s.L - s.T;
     auto pos_of = [&](int row) { return first + min(row, all_rows - 1) / a.g; };
     const int p0 = pos_of(row_from), p1 = pos_of(row_from + kBM - 1);       // the workgroup's
@@ -234,6 +263,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         store_v(0, 0, plain_to(0, ok4, p0, p1));
     }
     int page_next = look_up(min(1, tl.n - 1));
+    // the second wave of a SIMD goes first where both could: the two drift into
+    // opposite phases, one's products beside the other's softmax
+    if (__builtin_amdgcn_s_getreg(3 << 11 | 4) & 1) __builtin_amdgcn_s_setprio(1);
     for (int u = 0; u < tl.n; ++u) {
         __syncthreads();          // tile u is in its buffer, and the other one is done with
         const lds_t kb = (lds_t)&s_kv[u & 1][0][0], vb = (lds_t)&s_kv[u & 1][1][0];
@@ -367,12 +399,52 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// ---------------------------------------------------------------------------
+// The new tokens of prompts into their pages: one workgroup per token, 16
+// bytes a thread.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes) {
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+        // the request whose rows hold this one: the last that starts at or before it
+        int lo = 0, hi = a.n_seq;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.q_start[mid] <= row) lo = mid + 1;
+            else hi = mid;
+        }
+        const int b = lo - 1;
+        if (b < 0) continue;
+        const int from = a.q_start[b], to = a.q_start[b + 1], L = a.seq_len[b];
+        if (from < 0 || row >= to || to > a.n_rows || L < 0 || L > a.max_pages << a.ps_log2 ||
+            to - from > L)
+            continue;
+        const int j = (int)(L - (to - from) + (row - from));
+        const int page = a.table[(int64_t)b * a.max_pages + (j >> a.ps_log2)];
+        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
+        const int in = j & ((1 << a.ps_log2) - 1);
+        const int all = a.n_kv * row_bytes;               // bytes of one token's keys
+        char* base = a.kv + (int64_t)page * a.page_stride;
+        for (int x = threadIdx.x * 16; x < 2 * all; x += kThreads * 16) {
+            const int y = x < all ? x : x - all;
+            const int head = y / row_bytes, d = y - head * row_bytes;
+            const char* src = (x < all ? a.kn : a.vn) + row * a.kv_stride + y;
+            char* dst = base + ((int64_t)((x < all ? 0 : a.n_kv) + head) << a.ps_log2) * row_bytes +
+                        (int64_t)in * row_bytes + d;
+            *(u32x4*)dst = *(const u32x4*)src;
+        }
+    }
+}
+
 template <int D>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
     // blocks of rows: every request has one that is not full at most
     const int64_t blocks = (int64_t)a.n_rows * a.g / kBM + a.n_seq;
     const int64_t grid = blocks * a.n_kv;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(store_tokens_kernel, dim3(a.n_rows < 4096 ? a.n_rows : 4096),
+                       dim3(kThreads), 0, stream, a, 2 * D);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_tiles_kernel<D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
                        a);
     return hipGetLastError();
