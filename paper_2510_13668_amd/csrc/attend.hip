@@ -66,16 +66,22 @@ struct Half {
     bool ok;
 };
 
-template <int kDtype, int D>
+// A lane's share of a V row.  Values that one block alone reads pass the caches
+// by, whole lines at a time (128 requests: 382 -> 364 us, 6.0 TB/s; two long
+// ones 75.5 -> 67.7; where several blocks read them, 76 -> 93); keys take two
+// instructions a line, which only the cache joins (the same for them: 364 ->
+// 383).
+template <int kDtype, int D, bool kOnce>
 __device__ inline void load_row(const char* p, uint32_t* to) {
     constexpr int n = Tile<kDtype, D>::kRowV;
     if constexpr (n == 8) {
-        const u32x2 x = *(const u32x2*)p;
+        const u32x2 x = kOnce ? __builtin_nontemporal_load((const u32x2*)p) : *(const u32x2*)p;
         to[0] = x[0], to[1] = x[1];
     } else {
 #pragma unroll
         for (int i = 0; i < n / 16; ++i) {
-            const u32x4 x = *(const u32x4*)(p + 16 * i);
+            const u32x4* at = (const u32x4*)(p + 16 * i);
+            const u32x4 x = kOnce ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
             for (int w = 0; w < 4; ++w) to[4 * i + w] = x[w];
         }
@@ -157,6 +163,25 @@ __device__ inline float value_at(const uint32_t* w, int i) {
     return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
 
+// n outputs of one row
+template <int kDtype, int n>
+__device__ inline void store_out(char* to, const float* y) {
+#pragma unroll
+    for (int i = 0; i < n; i += 4) {
+        if constexpr (kDtype == STAR_BF16)
+            *(u32x2*)(to + 2 * i) =
+                u32x2{pack_bf16x2_rne(y[i], y[i + 1]), pack_bf16x2_rne(y[i + 2], y[i + 3])};
+        else
+            *(f32x4*)(to + 4 * i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    }
+}
+// a / b of two counts: 64-bit divisions, a hundred instructions and more each,
+// only where the counts need them
+__device__ inline int64_t quotient(int64_t a, int64_t b) {
+    if ((a | b) >> 32) return a / b;
+    return (uint32_t)a / (uint32_t)b;
+}
+
 // ---------------------------------------------------------------------------
 // The row-block kernel: any lengths, group sizes, masks and both types.
 //
@@ -170,7 +195,7 @@ __device__ inline float value_at(const uint32_t* w, int i) {
 // do not depend on the order of arrival.  Keys and values are read once (16
 // rows or fewer a head), registers to registers; HBM bounds it.
 // ---------------------------------------------------------------------------
-template <int kDtype, int D>
+template <int kDtype, int D, bool kOnce>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
     using TT = Tile<kDtype, D>;
     constexpr int kB = TT::kB, kT = TT::kT, E = TT::E;
@@ -178,8 +203,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
     constexpr int kPart = kRows * D + 4 * kRows;       // floats of one part
     __shared__ float s_o[kWaves][kRows][D + 4];
     __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
-    __shared__ int64_t s_tmp[kWaves + 1], s_base;
-    __shared__ int s_b;
+    __shared__ int64_t s_tmp[2 * kWaves], s_steps[kThreads + 1], s_short[kThreads + 1];
+    __shared__ Slot s_slot[kThreads];
     __shared__ uint32_t s_ticket;
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -187,52 +212,114 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
     const int r = lane & 15, c = lane >> 4;
     const int wg = blockIdx.x;
 
-    // this workgroup's piece of all steps
+    // steps of all blocks, and how many blocks have one step (`per` requests a
+    // thread)
     const int per = (a.n_seq + kThreads - 1) / kThreads;
     int32_t bad = 0;
-    int64_t mine = 0, total;
-    for (int b = tid * per; b < min(a.n_seq, (tid + 1) * per); ++b) {
-        const Slot s = slot_of<kT>(a, b, bad);
-        mine += (int64_t)a.n_kv * s.blocks * s.steps;
-    }
-    if (wg == 0) report_error(a.err, bad);
-    const int64_t before = block_exclusive_scan_i64<kThreads>(mine, OpAdd(), 0, s_tmp, &total);
-    const int64_t piece = max((int64_t)a.min_steps, ceil_div(total, gridDim.x));
-    int64_t u = wg * piece;
-    if (u >= total) return;
-    const int64_t end = min(total, u + piece);
-    if (before <= u && u < before + mine) {
-        int64_t base = before;
-        for (int b = tid * per;; ++b) {
+    {
+        int64_t steps = 0, one = 0;
+        for (int b = tid * per; b < min(a.n_seq, (tid + 1) * per); ++b) {
             const Slot s = slot_of<kT>(a, b, bad);
-            const int64_t n = (int64_t)a.n_kv * s.blocks * s.steps;
-            if (u < base + n) {
-                s_b = b;
-                s_base = base;
+            if (per == 1) s_slot[tid] = s;
+            const int64_t blocks = (int64_t)a.n_kv * s.blocks;
+            steps += blocks * s.steps;
+            one += s.steps == 1 ? blocks : 0;
+        }
+        if (wg == 0) report_error(a.err, bad);
+        int64_t x = steps, y = one;
+        block_incl_add2_i64<kThreads>(x, y, s_tmp);
+        s_steps[tid] = x - steps, s_short[tid] = y - one;
+        if (tid == kThreads - 1) s_steps[kThreads] = x, s_short[kThreads] = y;
+        __syncthreads();
+    }
+    // Where they fill the chip by themselves, blocks of one step are a wave's
+    // each (in batches of short requests three waves of four had no tile, and
+    // every block cost a meeting: 512 requests of 30 tokens took 45 us, now 20)
+    const int64_t n_short = s_short[kThreads] >= 2 * gridDim.x ? s_short[kThreads] : 0;
+    const bool alone_too = n_short > 0;
+    // the request that holds step (or one-step block) `at`, and its first
+    struct Place {
+        Slot s;
+        int b;
+        int64_t base, n;
+    };
+    auto find = [&](int64_t at, bool one) {
+        auto before = [&](int i) {
+            return one ? s_short[i] : s_steps[i] - (alone_too ? s_short[i] : 0);
+        };
+        auto width = [&](const Slot& s) {
+            const int64_t blocks = (int64_t)a.n_kv * s.blocks;
+            return one ? (s.steps == 1 ? blocks : 0)
+                       : alone_too && s.steps == 1 ? 0 : blocks * s.steps;
+        };
+        int chunk = -1;                  // the last that starts at or before `at`
+        for (int q = 0; q < min(a.n_seq, kThreads); q += kWave)
+            chunk += __popcll(__ballot(q + lane < a.n_seq && before(q + lane) <= at));
+        chunk = __builtin_amdgcn_readfirstlane(chunk);
+        Place x;
+        x.base = readlane_i64(before(chunk), 0);
+        if (per == 1) {
+            x.b = chunk;
+            x.s.L = __builtin_amdgcn_readfirstlane(s_slot[chunk].L);
+            x.s.T = __builtin_amdgcn_readfirstlane(s_slot[chunk].T);
+            x.s.row0 = __builtin_amdgcn_readfirstlane(s_slot[chunk].row0);
+            x.s.blocks = __builtin_amdgcn_readfirstlane(s_slot[chunk].blocks);
+            x.s.steps = __builtin_amdgcn_readfirstlane(s_slot[chunk].steps);
+            x.n = width(x.s);
+            return x;
+        }
+        x.n = 0;
+        x.b = 0;
+        x.s = Slot{0, 0, 0, 0, 0};
+        const int end = min(a.n_seq, (chunk + 1) * per);
+        for (int from = chunk * per; from < end; from += kWave) {
+            Slot s = {0, 0, 0, 0, 0};
+            int32_t ignored = 0;
+            if (from + lane < end) s = slot_of<kT>(a, from + lane, ignored);
+            const int64_t mine = width(s);
+            const int64_t upto = wave_incl_add_i64(mine);
+            const uint64_t past = __ballot(x.base + upto > at);
+            if (past) {
+                const int i = __builtin_ctzll(past);
+                x.b = from + i;
+                x.base += readlane_i64(upto - mine, i);
+                x.n = readlane_i64(mine, i);
+                x.s.L = __builtin_amdgcn_readlane(s.L, i);
+                x.s.T = __builtin_amdgcn_readlane(s.T, i);
+                x.s.row0 = __builtin_amdgcn_readlane(s.row0, i);
+                x.s.blocks = __builtin_amdgcn_readlane(s.blocks, i);
+                x.s.steps = __builtin_amdgcn_readlane(s.steps, i);
                 break;
             }
-            base += n;
+            x.base += readlane_i64(upto, kWave - 1);
         }
-    }
-    __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(s_b);
-    int64_t base = readlane_i64(s_base, 0);
+        return x;
+    };
+
+    // this workgroup's piece of the other blocks' steps
+    const int64_t total = s_steps[kThreads] - n_short;
+    const int64_t piece = max((int64_t)a.min_steps, quotient(total + gridDim.x - 1, gridDim.x));
+    int64_t u = wg * piece;
+    const int64_t end = min(total, u + piece);
+    int64_t k = wg + (int64_t)wave * gridDim.x;          // this wave's next one-step block
     int32_t err = 0;
+    Place at_slot;
+    at_slot.base = at_slot.n = 0;
 
     const __amdgpu_buffer_rsrc_t part =
         xch_rsrc(a.part, (uint32_t)(2 * gridDim.x * kPart * sizeof(float)));
-    while (u < end) {
-        Slot s = slot_of<kT>(a, b, bad);
-        int64_t n_slot = (int64_t)a.n_kv * s.blocks * s.steps;
-        while (u >= base + n_slot) {
-            base += n_slot;
-            s = slot_of<kT>(a, ++b, bad);
-            n_slot = (int64_t)a.n_kv * s.blocks * s.steps;
-        }
-        const int item = (int)((u - base) / s.steps);
+    for (;;) {
+        const bool together = u < end;                   // all four waves, else one
+        if (!together && k >= n_short) break;
+        if (!together || u >= at_slot.base + at_slot.n)
+            at_slot = find(together ? u : k, !together);
+        const Slot s = at_slot.s;
+        const int b = at_slot.b;
+        const int64_t base = at_slot.base;
+        const int item = together ? (int)quotient(u - base, s.steps) : (int)(k - base);
         const int64_t item_u = base + (int64_t)item * s.steps;
-        const int step0 = (int)(u - item_u);
-        const int steps = (int)min((int64_t)(s.steps - step0), end - u);
+        const int step0 = together ? (int)(u - item_u) : 0;
+        const int steps = together ? (int)min((int64_t)(s.steps - step0), end - u) : 1;
         const int head = item / s.blocks, row_from = (item - head * s.blocks) * kRows;
         const int rows = min(s.T * a.g - row_from, kRows);
 
@@ -293,14 +380,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
                     load_k<kDtype, D>(row_at(kn, j + r, kb), c, f.k[h]);
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        load_row<kDtype, D>(row_at(vn + r * TT::kRowV, j + 4 * c + x,
+                        load_row<kDtype, D, kOnce>(row_at(vn + r * TT::kRowV, j + 4 * c + x,
                                                    vb + x * (D * kB)),
                                             f.v[4 * h + x]);
                 } else {
                     load_k<kDtype, D>(kb, c, f.k[h]);
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        load_row<kDtype, D>(vb + x * (D * kB), f.v[4 * h + x]);
+                        load_row<kDtype, D, kOnce>(vb + x * (D * kB), f.v[4 * h + x]);
                 }
             }
         };
@@ -310,15 +397,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
         for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         float m = -INFINITY, l = 0.0f;                   // l: this lane's tokens only
 
+        const int t_step = together ? kWaves : 1;
         const int t_end = min(tl.n, kWaves * (step0 + steps));
-        int t = kWaves * step0 + wave;
+        int t = together ? kWaves * step0 + wave : 0;
         TT f;
         Half hf[TT::kHalves];
         if (t < t_end) load(tl.at(t), f, hf);
-        for (; t < t_end; t += kWaves) {
+        for (; t < t_end; t += t_step) {
             TT nf;
             Half nh[TT::kHalves];
-            if (kAhead && t + kWaves < t_end) load(tl.at(t + kWaves), nf, nh);
+            if (kAhead && t + t_step < t_end) load(tl.at(t + t_step), nf, nh);
 
             const int j0 = tl.at(t) * kT;
             float p[4 * TT::kHalves];
@@ -412,8 +500,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
                 f = nf;
 #pragma unroll
                 for (int h = 0; h < TT::kHalves; ++h) hf[h] = nh[h];
-            } else if (t + kWaves < t_end) {
-                load(tl.at(t + kWaves), f, hf);
+            } else if (t + t_step < t_end) {
+                load(tl.at(t + t_step), f, hf);
             }
         }
 
@@ -422,7 +510,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
         if (step0 == 0 && s.L > 0) {
             const int i0 = (row_from + a.g - 1) / a.g, i1 = (row_from + rows - 1) / a.g;
             constexpr int kPer = D * kB / 16;             // 16-byte pieces of a row
-            for (int x = tid; x < (i1 - i0 + 1) * 2 * kPer; x += kThreads) {
+            for (int x = together ? tid : lane; x < (i1 - i0 + 1) * 2 * kPer;
+                 x += together ? kThreads : kWave) {
                 const int i = i0 + x / (2 * kPer), d = x % kPer * 16, j = first + i;
                 const bool value = x / kPer & 1;
                 const int page = pages[j >> a.ps_log2];
@@ -435,8 +524,27 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
             }
         }
 
-        // the four waves' parts meet: thread (row, 16 of them) sums E outputs
         l = quad_sum(l);
+        if (!together) {
+            // lane (r, c) has row r's outputs 4c E .. 4 (c + 1) E - 1
+            if (r < rows) {
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees nothing is 0
+                const int64_t at = q_row * a.n_heads + q_head;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float y[E];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) y[i] = o[i][x] * inv;
+                    store_out<kDtype, E>(a.out + (at * D + (4 * c + x) * E) * kB, y);
+                }
+                if (a.lse && c == 0)
+                    a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+            }
+            k += (int64_t)kWaves * gridDim.x;
+            continue;
+        }
+
+        // the four waves' parts meet: thread (row, 16 of them) sums E outputs
         if (c == 0) s_m[wave][r] = m, s_l[wave][r] = l;
 #pragma unroll
         for (int x = 0; x < 4; ++x)
@@ -462,43 +570,87 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
         if (steps < s.steps) {
             // a part of a block: its place goes by the workgroup that holds it
             // (the block's first part after that workgroup's own first)
-            const int w0 = (int)(item_u / piece), w1 = (int)((item_u + s.steps - 1) / piece);
+            const int w0 = (int)quotient(item_u, piece);
+            const int w1 = (int)quotient(item_u + s.steps - 1, piece);
             auto part_at = [&](int w) {
                 return (uint32_t)((2 * w + (w == w0)) * kPart * sizeof(float));
             };
             const uint32_t off = part_at(wg);
-            if ((tid & 15) == 0)
-                xch_store(u32x4{__float_as_uint(jm), __float_as_uint(jl), 0, 0}, part,
-                          off + jr * 16);
-            // (maximum and sum take the 16 bytes of two floats each and padding)
+            if (jr < rows) {
+                if ((tid & 15) == 0)
+                    xch_store(u32x4{__float_as_uint(jm), __float_as_uint(jl), 0, 0}, part,
+                              off + jr * 16);
 #pragma unroll
-            for (int i = 0; i < E; i += 4)
-                xch_store(u32x4{__float_as_uint(jo[i]), __float_as_uint(jo[i + 1]),
-                                __float_as_uint(jo[i + 2]), __float_as_uint(jo[i + 3])},
-                          part, off + kRows * 16 + (jr * D + jd + i) * 4);
+                for (int i = 0; i < E; i += 4)
+                    xch_store(u32x4{__float_as_uint(jo[i]), __float_as_uint(jo[i + 1]),
+                                    __float_as_uint(jo[i + 2]), __float_as_uint(jo[i + 3])},
+                              part, off + kRows * 16 + (jr * D + jd + i) * 4);
+            }
             xch_wait_stores();
             write = xch_last_arrival(a.tickets + w0, (uint32_t)(w1 - w0 + 1), &s_ticket);
             if (write) {
+                // In order, several parts' loads in flight, and where the block
+                // has few rows, the threads of the others take every second (4th,
+                // ..) part: one at a time cost 0.5 us each, 30 us for a long cache
+                // cut 64 times
+                constexpr int kBatch = D == 64 ? 4 : 2;
+                const int lg = rows > 8 ? 4 : rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0;
+                const int groups = kRows >> lg, group = jr >> lg, pr = jr & ((1 << lg) - 1);
                 jm = -INFINITY, jl = 0.0f;
 #pragma unroll
                 for (int i = 0; i < E; ++i) jo[i] = 0.0f;
-                for (int w = w0; w <= w1; ++w) {
-                    const uint32_t at = part_at(w);
-                    const u32x4 ml = xch_load(part, at + jr * 16);
-                    u32x4 v[E / 4];
+                for (int w = w0 + group; w <= w1; w += kBatch * groups) {
+                    u32x4 ml[kBatch], v[kBatch][E / 4];
 #pragma unroll
-                    for (int i = 0; i < E; i += 4)
-                        v[i / 4] = xch_load(part, at + kRows * 16 + (jr * D + jd + i) * 4);
-                    const float pm = __uint_as_float(ml[0]), pl = __uint_as_float(ml[1]);
-                    const float nm = fmaxf(jm, pm);
-                    jref = nm == -INFINITY ? 0.0f : nm;
+                    for (int x = 0; x < kBatch; ++x) {
+                        const int wx = w + x * groups;
+                        const uint32_t at = wx <= w1 ? part_at(wx) : kXchOob;
+                        ml[x] = xch_load(part, at + pr * 16);
+#pragma unroll
+                        for (int i = 0; i < E; i += 4)
+                            v[x][i / 4] = xch_load(part, at + kRows * 16 + (pr * D + jd + i) * 4);
+                    }
+                    float top = jm;
+#pragma unroll
+                    for (int x = 0; x < kBatch; ++x)
+                        if (w + x * groups <= w1) top = fmaxf(top, __uint_as_float(ml[x][0]));
+                    jref = top == -INFINITY ? 0.0f : top;
                     const float f0 = __builtin_amdgcn_exp2f(jm - jref);
-                    const float f1 = __builtin_amdgcn_exp2f(pm - jref);
-                    jm = nm;
-                    jl = jl * f0 + pl * f1;
+                    jm = top;
+                    jl *= f0;
 #pragma unroll
-                    for (int i = 0; i < E; ++i)
-                        jo[i] = jo[i] * f0 + __uint_as_float(v[i / 4][i & 3]) * f1;
+                    for (int i = 0; i < E; ++i) jo[i] *= f0;
+#pragma unroll
+                    for (int x = 0; x < kBatch; ++x) {
+                        if (w + x * groups > w1) break;
+                        const float f1 = __builtin_amdgcn_exp2f(__uint_as_float(ml[x][0]) - jref);
+                        jl += __uint_as_float(ml[x][1]) * f1;
+#pragma unroll
+                        for (int i = 0; i < E; ++i)
+                            jo[i] += __uint_as_float(v[x][i / 4][i & 3]) * f1;
+                    }
+                }
+                if (groups > 1) {
+                    // (every thread has read the waves' parts: the meeting is past)
+                    if ((tid & 15) == 0) s_m[0][jr] = jm, s_l[0][jr] = jl;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) s_o[0][jr][jd + i] = jo[i];
+                    __syncthreads();
+                    if (jr < rows) {
+                        for (int x = 1; x < groups; ++x) jm = fmaxf(jm, s_m[0][(x << lg) + jr]);
+                        jref = jm == -INFINITY ? 0.0f : jm;
+                        jl = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < E; ++i) jo[i] = 0.0f;
+                        for (int x = 0; x < groups; ++x) {
+                            const float f1 =
+                                __builtin_amdgcn_exp2f(s_m[0][(x << lg) + jr] - jref);
+                            jl += f1 * s_l[0][(x << lg) + jr];
+#pragma unroll
+                            for (int i = 0; i < E; ++i)
+                                jo[i] += f1 * s_o[0][(x << lg) + jr][jd + i];
+                        }
+                    }
                 }
             }
         }
@@ -506,21 +658,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
             const int wr = row_from + jr;
             const int64_t at = (int64_t)(s.row0 + wr / a.g) * a.n_heads + head * a.g + wr % a.g;
             const float inv = jl == 0.0f ? 0.0f : 1.0f / jl;   // a row that sees nothing is 0
-            char* to = a.out + (at * D + jd) * kB;
-            if constexpr (kDtype == STAR_BF16) {
 #pragma unroll
-                for (int i = 0; i < E; i += 4) {
-                    u32x2 x;
-                    x[0] = pack_bf16x2_rne(jo[i] * inv, jo[i + 1] * inv);
-                    x[1] = pack_bf16x2_rne(jo[i + 2] * inv, jo[i + 3] * inv);
-                    *(u32x2*)(to + i * kB) = x;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < E; i += 4)
-                    *(f32x4*)(to + i * kB) =
-                        f32x4{jo[i] * inv, jo[i + 1] * inv, jo[i + 2] * inv, jo[i + 3] * inv};
-            }
+            for (int i = 0; i < E; ++i) jo[i] *= inv;
+            store_out<kDtype, E>(a.out + (at * D + jd) * kB, jo);
             if (a.lse && (tid & 15) == 0)
                 a.lse[at] = jl == 0.0f ? -INFINITY : (jm + __builtin_amdgcn_logf(jl)) * kLn2;
         }
@@ -532,7 +672,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
 
 template <int kDtype, int D>
 hipError_t launch_rows(const AttendArgs& a, int grid, hipStream_t stream) {
-    hipLaunchKernelGGL((attend_rows_kernel<kDtype, D>), dim3(grid), dim3(kThreads), 0, stream, a);
+    // one block a request and key-value head reads every key and value once
+    if (!a.q_start && a.g <= kRows)
+        hipLaunchKernelGGL((attend_rows_kernel<kDtype, D, true>), dim3(grid), dim3(kThreads), 0,
+                           stream, a);
+    else
+        hipLaunchKernelGGL((attend_rows_kernel<kDtype, D, false>), dim3(grid), dim3(kThreads), 0,
+                           stream, a);
     return hipGetLastError();
 }
 
@@ -543,7 +689,7 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     // two workgroups a CU (one where a row's 256 elements fill the registers)
     pl.grid = p.head_dim == 256 ? 256 : 512;
     static_assert(512 <= kMaxTickets, "one ticket per workgroup");
-    pl.min_steps = 2;
+    pl.min_steps = 1;
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
     const int64_t rows = (int64_t)p.n_rows * (p.n_heads / p.n_kv_heads);
     pl.tiled = !decode && p.dtype == STAR_BF16 && p.head_dim <= 128 &&

@@ -459,30 +459,26 @@ def attend_params(n_seq, n_rows, n_heads, n_kv_heads, head_dim, dtype, page_size
 _TORCH_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
 
-def _strided(t: torch.Tensor, dtype, shape, stride: int) -> int:
-    """The address of a tensor of `shape` that is dense but for its first
-    dimension, whose steps are `stride` elements."""
+def _strided(t: torch.Tensor, dtype, shape, strides) -> int:
+    """The address of a device tensor of this shape and these strides (the
+    steps of dimensions of size 1 are any)."""
     if not t.is_cuda:
         raise ValueError("libstar takes device tensors")
     if t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    got, dense = t.stride(), 1
-    for n, step in zip(reversed(shape[1:]), reversed(got[1:])):
-        if step != dense and n > 1:
-            raise ValueError("only the first dimension may have a stride of its own")
-        dense *= n
-    if shape[0] > 1 and got[0] != stride:
-        raise ValueError(f"a first stride of {got[0]}, the parameters say {stride}")
+        raise ValueError(f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    got = t.stride()
+    if got != strides and any(n > 1 and x != y for n, x, y in zip(shape, got, strides)):
+        raise ValueError(f"strides {got} where the parameters and a dense layout give {strides}")
     return t.data_ptr()
 
 
 def _attend_ptrs(p: AttendParams, q, k_new, v_new, kv):
-    dt, D = _TORCH_DTYPES[p.dtype], p.head_dim
-    new = (p.n_rows, p.n_kv_heads, D)
-    return (_strided(q, dt, (p.n_rows, p.n_heads, D), p.q_stride),
-            _strided(k_new, dt, new, p.kv_stride), _strided(v_new, dt, new, p.kv_stride),
-            _strided(kv, dt, (p.n_pages, 2, p.n_kv_heads, p.page_size, D),
-                     p.page_stride // dt.itemsize))
+    dt, D, n, Hkv, ps = _TORCH_DTYPES[p.dtype], p.head_dim, p.n_rows, p.n_kv_heads, p.page_size
+    new, rows = (n, Hkv, D), (p.kv_stride, D, 1)
+    return (_strided(q, dt, (n, p.n_heads, D), (p.q_stride, D, 1)),
+            _strided(k_new, dt, new, rows), _strided(v_new, dt, new, rows),
+            _strided(kv, dt, (p.n_pages, 2, Hkv, ps, D),
+                     (p.page_stride // dt.itemsize, Hkv * ps * D, ps * D, D, 1)))
 
 
 def attend_decode_workspace_size(p: AttendParams) -> int:

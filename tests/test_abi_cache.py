@@ -139,19 +139,19 @@ def test_attention_rejects_null_pointers_and_workspaces(L):
 
 def test_binding_checks_the_tensors():
     """Layouts that the pointers alone could not tell apart are refused."""
-    p = _attend(q_stride=12 * 128, kv_stride=12 * 128)
+    rows = (1536, 128, 1)
     fake = lambda *shape: _Meta(torch.empty(shape, dtype=torch.bfloat16))
     qkv = torch.empty((4, 12, 128), dtype=torch.bfloat16)
-    assert star._strided(_Meta(qkv[:, :8]), torch.bfloat16, (4, 8, 128), 1536) == qkv.data_ptr()
+    assert star._strided(_Meta(qkv[:, :8]), torch.bfloat16, (4, 8, 128), rows) == qkv.data_ptr()
     for bad in (fake(4, 8, 64), fake(4, 8, 128), _Meta(qkv[:, :8].float()),
                 _Meta(qkv.transpose(0, 1)[:8].transpose(0, 1)[:, :, :64]),
                 _Meta(torch.empty((4, 128, 8), dtype=torch.bfloat16).transpose(1, 2))):
         with pytest.raises(ValueError):
-            star._strided(bad, torch.bfloat16, (4, 8, 128), p.q_stride)
+            star._strided(bad, torch.bfloat16, (4, 8, 128), rows)
     with pytest.raises(ValueError):
-        star._strided(qkv[:, :8], torch.bfloat16, (4, 8, 128), 1536)       # not on a GPU
+        star._strided(qkv[:, :8], torch.bfloat16, (4, 8, 128), rows)       # not on a GPU
     one = _Meta(torch.empty((1, 8, 128), dtype=torch.bfloat16))             # one row: any stride
-    star._strided(one, torch.bfloat16, (1, 8, 128), 5)
+    star._strided(one, torch.bfloat16, (1, 8, 128), (5, 128, 1))
 
 
 class _Meta:
