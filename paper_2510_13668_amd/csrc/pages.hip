@@ -101,9 +101,14 @@ __device__ inline SlotPlan plan_slot(const AssignArgs& a, int b, int& need, int3
     return s;
 }
 
+// A wave's stretch of an instance's P pages, a multiple of 256.
+__device__ inline int stretch_of(int P) {
+    return ((P + kPlanWaves - 1) / kPlanWaves + 255) / 256 * 256;
+}
+
 __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a) {
-    __shared__ int s_count[kPlanWaves];
-    __shared__ int64_t s_tmp[kPlanWaves + 1];
+    __shared__ int s_count[kPlanWaves], s_copies;
+    __shared__ int64_t s_tmp[2 * kPlanWaves];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int P = a.n_pages / a.n_inst;
     if (blockIdx.x >= (unsigned)a.n_inst) {
@@ -115,111 +120,174 @@ __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a)
         return;
     }
     const int inst = blockIdx.x, page0 = inst * P;
+    const int32_t* refs = a.refs + page0;
+    if (tid == 0) s_copies = 0;
+
+    // Everything that depends on arrays alone is asked for first: the first
+    // stretch of counts, and this thread's first slot.
+    const int stretch = stretch_of(P);
+    const int from = min(P, wave * stretch), to = min(P, from + stretch);
+    constexpr int kHeld = 2;                    // counts kept in registers: 512 a wave
+    int held[kHeld][4];
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) load_counts(refs, from + 256 * h, to, lane, held[h]);
+    const int per = (a.n_seq + kPlanThreads - 1) / kPlanThreads;
+    const int b0 = min(a.n_seq, tid * per), b1 = min(a.n_seq, b0 + per);
+    int32_t bad = 0;
+    int need0 = 0;
+    SlotPlan slot0 = {};
+    slot0.inst = -1;
+    int64_t mine = 0, copying = 0;
+    for (int b = b0; b < b1; ++b) {
+        int need;
+        const SlotPlan s = plan_slot(a, b, need, bad);
+        if (b == b0) slot0 = s, need0 = need;
+        if (s.inst == inst) mine += need, copying += s.kept - s.shared;
+    }
 
     // the instance's free pages in order: each wave counts its stretch, then
     // writes it behind the waves before
-    const int stretch = ((P + kPlanWaves - 1) / kPlanWaves + 255) / 256 * 256;
-    const int from = min(P, wave * stretch), to = min(P, from + stretch);
     int n = 0;
-    for (int at = from; at < to; at += 256) {
+    for (int at = from, h = 0; at < to; at += 256, ++h) {
         int x[4];
-        load_counts(a.refs + page0, at, to, lane, x);
+        if (h >= kHeld) load_counts(refs, at, to, lane, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) n += __popcll(__ballot(x[k] == 0));
+        for (int k = 0; k < 4; ++k)
+            n += __popcll(__ballot((h == 0 ? held[0][k] : h == 1 ? held[1][k] : x[k]) == 0));
     }
     if (lane == 0) s_count[wave] = n;
-    __syncthreads();
+    int64_t upto = mine, k = copying;
+    block_incl_add2_i64<kPlanThreads>(upto, k, s_tmp);
+    upto -= mine, k -= copying;
     int n_free = 0, rank = 0;
     for (int w = 0; w < kPlanWaves; ++w) {
         if (w < wave) rank += s_count[w];
         n_free += s_count[w];
     }
     int32_t* list = a.free_list + page0;
-    for (int at = from; at < to; at += 256) {
+    for (int at = from, h = 0; at < to; at += 256, ++h) {
         int x[4];
-        load_counts(a.refs + page0, at, to, lane, x);
+        if (h >= kHeld) load_counts(refs, at, to, lane, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint64_t mask = __ballot(x[k] == 0);
-            if (x[k] == 0) list[rank + lanes_below(mask, lane)] = page0 + at + k * kWave + lane;
+        for (int j = 0; j < 4; ++j) {
+            const bool free = (h == 0 ? held[0][j] : h == 1 ? held[1][j] : x[j]) == 0;
+            const uint64_t mask = __ballot(free);
+            if (free) list[rank + lanes_below(mask, lane)] = page0 + at + j * kWave + lane;
             rank += __popcll(mask);
         }
     }
+    __syncthreads();           // the list is written (the copies read it)
 
-    // the instance's slots in order take them
-    const int per = (a.n_seq + kPlanThreads - 1) / kPlanThreads;
-    const int b0 = min(a.n_seq, tid * per), b1 = min(a.n_seq, b0 + per);
-    int32_t bad = 0;
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) {
-        int need;
-        const SlotPlan s = plan_slot(a, b, need, bad);
-        if (s.inst == inst) mine += need;
-    }
-    __syncthreads();           // the list is written
-    int64_t upto = block_exclusive_scan_i64<kPlanThreads>(mine, OpAdd(), 0, s_tmp, nullptr);
-    int64_t copying = 0;
-    for (int b = b0; b < b1; ++b) {
-        int need;
-        SlotPlan s = plan_slot(a, b, need, bad);
-        if (s.inst != inst && !(s.inst < 0 && inst == 0)) continue;
-        if (s.inst == inst) {
-            s.first = (int)min(upto, (int64_t)P);
-            upto += need;
-            if (need > 0 && upto > n_free) s.served = 0, bad |= STAR_DEV_NO_PAGES;
-            if (s.served) copying += s.kept - s.shared;
+    // Its slots in order take them.  Running demands only grow, so the slots
+    // served come before all those that are not: their running counts of
+    // copies need no second pass
+    int last_copy = 0;
+    for (int i = 0; i < per; ++i) {
+        const int b = b0 + i;
+        int copies = 0;
+        SlotPlan s = slot0;
+        if (b < b1) {
+            int need = need0;
+            if (i > 0) s = plan_slot(a, b, need, bad);
+            if (s.inst == inst) {
+                s.first = (int)min(upto, (int64_t)P);
+                upto += need;
+                if (need > 0 && upto > n_free) s.served = 0, bad |= STAR_DEV_NO_PAGES;
+                if (s.served) copies = s.kept - s.shared;
+            }
+            if (s.inst == inst || (s.inst < 0 && inst == 0)) a.plan[b] = s;
         }
-        a.plan[b] = s;
-    }
-    int64_t all = 0;
-    int64_t k = block_exclusive_scan_i64<kPlanThreads>(copying, OpAdd(), 0, s_tmp, &all);
-    if (tid == 0) a.n_copies[inst] = (int)all;
-    if (copying) {
-        for (int b = b0; b < b1; ++b) {
-            const SlotPlan s = a.plan[b];          // this thread's own
-            if (s.inst != inst || !s.served) continue;
-            const int32_t* row = a.table + (int64_t)s.from * a.max_pages;
-            for (int j = s.shared; j < s.kept; ++j, ++k) {
+        // A slot's copies go on the list: a few (a fork's last page) by its own
+        // thread, more by its wave, 64 pages at once
+        constexpr int kFew = 4;
+        if (copies > 0 && copies <= kFew) {
+            const int32_t* row = a.table + (int64_t)s.from * a.max_pages + s.shared;
+            for (int j = 0; j < copies; ++j) {
                 int src = row[j];
                 if ((uint32_t)src >= (uint32_t)a.n_pages) src = -1, bad |= STAR_DEV_BAD_PAGE;
-                a.copies[2 * (page0 + k)] = src;
-                a.copies[2 * (page0 + k) + 1] = list[s.first + j - s.shared];
+                a.copies[2 * (page0 + k + j)] = src;
+                a.copies[2 * (page0 + k + j) + 1] = list[s.first + j];
             }
         }
+        for (uint64_t todo = __ballot(copies > kFew); todo; todo &= todo - 1) {
+            const int x = __builtin_ctzll(todo);
+            const int count = __builtin_amdgcn_readlane(copies, x);
+            const int shared = __builtin_amdgcn_readlane(s.shared, x);
+            const int first = __builtin_amdgcn_readlane(s.first, x);
+            const int at = __builtin_amdgcn_readlane((int)k, x);
+            const int32_t* row =
+                a.table + (int64_t)__builtin_amdgcn_readlane(s.from, x) * a.max_pages + shared;
+            for (int j = lane; j < count; j += kWave) {
+                int src = row[j];
+                if ((uint32_t)src >= (uint32_t)a.n_pages) src = -1, bad |= STAR_DEV_BAD_PAGE;
+                a.copies[2 * (page0 + at + j)] = src;
+                a.copies[2 * (page0 + at + j) + 1] = list[first + j];
+            }
+        }
+        k += copies;
+        if (copies) last_copy = (int)k;
     }
+    if (last_copy) atomicMax(&s_copies, last_copy);
+    __syncthreads();
+    if (tid == 0) a.n_copies[inst] = s_copies;
     report_error(a.err, bad);
 }
 
 // Page copies: source and target pages of every instance's list, in all
-// layers; 16 bytes a thread and load, eight loads in flight.
+// layers, kLanes threads a page and layer; 16 bytes a thread and load, eight
+// loads in flight.  Nothing copied is read again here, so it passes the caches
+// by (917 KB pages: 187 -> 176 us; migrations 82 -> 73).
+template <int kLanes>
+__device__ inline void copy_pages_by(char* kv, const int32_t* copies, const int32_t* n_copies,
+                                     int n_inst, int P, int n_layers, int64_t page_bytes,
+                                     int64_t page_stride, int64_t layer_stride, int worker,
+                                     int workers) {
+    constexpr int kTeams = kRunThreads / kLanes;
+    int64_t item = (int64_t)worker * kTeams + threadIdx.x / kLanes, base = 0;
+    for (int i = 0; i < n_inst; ++i) {
+        const int64_t n = (int64_t)n_copies[i] * n_layers;
+        for (; item < base + n; item += (int64_t)workers * kTeams) {
+            const int64_t x = item - base;
+            const int64_t k = (x >> 32 ? x / n_layers : (uint32_t)x / (uint32_t)n_layers);
+            const int layer = (int)(x - k * n_layers);
+            const u32x2 pair = *(const u32x2*)(copies + 2 * (k + (int64_t)i * P));
+            const int src = (int)pair[0], dst = (int)pair[1];
+            if (src < 0) continue;
+            const char* from = kv + layer * layer_stride + src * page_stride;
+            char* to = kv + layer * layer_stride + dst * page_stride;
+            constexpr int kStep = kLanes * 16, kUnroll = 8;
+            int64_t at = threadIdx.x % kLanes * 16;
+            for (; at + (kUnroll - 1) * kStep < page_bytes; at += kUnroll * kStep) {
+                u32x4 v[kUnroll];
+#pragma unroll
+                for (int q = 0; q < kUnroll; ++q)
+                    v[q] = __builtin_nontemporal_load((const u32x4*)(from + at + q * kStep));
+#pragma unroll
+                for (int q = 0; q < kUnroll; ++q)
+                    __builtin_nontemporal_store(v[q], (u32x4*)(to + at + q * kStep));
+            }
+            for (; at < page_bytes; at += kStep)
+                __builtin_nontemporal_store(__builtin_nontemporal_load((const u32x4*)(from + at)),
+                                            (u32x4*)(to + at));
+        }
+        base += n;
+    }
+}
+// A small page is a few lanes' or a wave's, so that many are in flight: each
+// waits for its place in the list first (1440-byte pages: 147 -> 69 us).
 __device__ inline void copy_pages(char* kv, const int32_t* copies, const int32_t* n_copies,
                                   int n_inst, int P, int n_layers, int64_t page_bytes,
                                   int64_t page_stride, int64_t layer_stride, int worker,
                                   int workers) {
-    int64_t item = worker, base = 0;
-    for (int i = 0; i < n_inst; ++i) {
-        const int64_t n = (int64_t)n_copies[i] * n_layers;
-        for (; item < base + n; item += workers) {
-            const int64_t x = item - base;
-            const int layer = (int)(x % n_layers);
-            const int64_t k = x / n_layers + (int64_t)i * P;
-            const int src = copies[2 * k], dst = copies[2 * k + 1];
-            if (src < 0) continue;
-            const char* from = kv + layer * layer_stride + src * page_stride;
-            char* to = kv + layer * layer_stride + dst * page_stride;
-            constexpr int kStep = kRunThreads * 16, kUnroll = 8;
-            int64_t at = threadIdx.x * 16;
-            for (; at + (kUnroll - 1) * kStep < page_bytes; at += kUnroll * kStep) {
-                u32x4 v[kUnroll];
-#pragma unroll
-                for (int q = 0; q < kUnroll; ++q) v[q] = *(const u32x4*)(from + at + q * kStep);
-#pragma unroll
-                for (int q = 0; q < kUnroll; ++q) *(u32x4*)(to + at + q * kStep) = v[q];
-            }
-            for (; at < page_bytes; at += kStep) *(u32x4*)(to + at) = *(const u32x4*)(from + at);
-        }
-        base += n;
-    }
+    if (page_bytes <= 512)
+        copy_pages_by<8>(kv, copies, n_copies, n_inst, P, n_layers, page_bytes, page_stride,
+                         layer_stride, worker, workers);
+    else if (page_bytes <= 8192)
+        copy_pages_by<64>(kv, copies, n_copies, n_inst, P, n_layers, page_bytes, page_stride,
+                          layer_stride, worker, workers);
+    else
+        copy_pages_by<256>(kv, copies, n_copies, n_inst, P, n_layers, page_bytes, page_stride,
+                           layer_stride, worker, workers);
 }
 
 __global__ __launch_bounds__(kRunThreads) void assign_run_kernel(AssignArgs a, int row_groups) {
@@ -284,7 +352,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int P = a.n_pages / a.n_inst, inst = blockIdx.x, page0 = inst * P;
     const int32_t* refs = a.refs + page0;
-    const int stretch = ((P + kPlanWaves - 1) / kPlanWaves + 255) / 256 * 256;
+    const int stretch = stretch_of(P);
     const int from = min(P, wave * stretch), to = min(P, from + stretch);
     int n = 0;
     for (int at = from; at < to; at += 256) {
