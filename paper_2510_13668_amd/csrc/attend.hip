@@ -692,7 +692,7 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     pl.min_steps = 1;
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
     const int64_t rows = (int64_t)p.n_rows * (p.n_heads / p.n_kv_heads);
-    pl.tiled = !decode && p.dtype == STAR_BF16 && p.head_dim <= 128 &&
+    pl.tiled = !decode && p.dtype == STAR_BF16 &&
                rows >= 64 * (int64_t)p.n_seq;
     return pl;
 }

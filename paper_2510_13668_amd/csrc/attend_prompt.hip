@@ -11,7 +11,6 @@ namespace star {
 namespace {
 
 constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
-constexpr int kBN = 64;          // tokens of a tile, 16 a wave to load
 constexpr int kThreads = 256, kWaves = 4;
 constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may lag
 
@@ -20,11 +19,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <int D>
 struct Lay {
+    // tokens of a tile, a quarter a wave to load (256 wide, the registers hold
+    // 32 tokens' scores beside the output)
+    static constexpr int kBN = D == 256 ? 32 : 64;
+    static constexpr int kPages = kBN / 16;       // sixteens of tokens, each in one page
+    static constexpr int kLoadRows = kBN / 4;     // tokens that a wave loads
     static constexpr int kRow = 2 * D;            // bytes of a token's keys (or values)
     static constexpr int kChunks = kRow / 16;     // 16-byte chunks of a row
     static constexpr int kTile = kBN * kRow;      // bytes of a tile's keys
     static constexpr int kRowsPerLoad = 1024 / kRow;
-    static constexpr int kLoads = 16 / kRowsPerLoad;   // 1 KiB loads of 16 tokens
+    static constexpr int kLoads = kLoadRows / kRowsPerLoad;   // 1 KiB loads of those
     // Chunk c of row r lies at chunk c ^ f(r) of the row.  Keys: 16 lanes read
     // one chunk of 16 rows; values: 32 lanes read 32 bytes of 4 rows and the 32
     // bytes beside; either way every bank is read once.
@@ -55,6 +59,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     using Y = Lay<D>;
     constexpr int kSteps = D / 16;       // contraction steps of a score
     constexpr int kOut = D / 32;         // 32-wide blocks of the output
+    constexpr int kBN = Y::kBN;
     __shared__ __attribute__((aligned(1024))) char s_kv[2][2][Y::kTile];
     __shared__ int64_t s_tmp[kWaves + 1];
     __shared__ int s_slot[2], s_fix[2];
@@ -160,19 +165,19 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int64_t head_off = (int64_t)head * Y::kRow << a.ps_log2;
     int32_t err = 0;
 
-    // lane x % 4's sixteen tokens of a tile: their page, or -1 where no row of
+    // lane x % kPages' sixteen tokens of a tile: their page, or -1 where no row of
     // the workgroup sees one of them; a bad page reports and reads page 0
     struct Pages {
         int page;
         bool ok;
     };
     auto look_up = [&](int u) {
-        const int j = tl.at(u) * kBN + 16 * (lane & 3);
+        const int j = tl.at(u) * kBN + 16 * (lane & (Y::kPages - 1));
         const bool seen = j <= p1 && (!a.window || j + 15 > p0 - a.window || j < a.sinks);
         return seen ? pages[j >> a.ps_log2] : -1;
     };
     auto check = [&](int u, int page) {
-        const int j = tl.at(u) * kBN + 16 * (lane & 3);
+        const int j = tl.at(u) * kBN + 16 * (lane & (Y::kPages - 1));
         const bool seen = j <= p1 && (!a.window || j + 15 > p0 - a.window || j < a.sinks);
         Pages x;
         x.ok = seen && (uint32_t)page < (uint32_t)a.n_pages;
@@ -180,14 +185,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         x.page = x.ok ? page : 0;
         return x;
     };
-    // this wave's sixteen tokens of a tile: keys and values into registers,
+    // this wave's tokens of a tile: keys and values into registers,
     // and from there into a buffer once the one before it is done with
     const int st_row = lane / Y::kChunks, st_ch = lane % Y::kChunks;
     const int g_off = st_row * Y::kRow + st_ch * 16;
     u32x4 next_k[Y::kLoads], next_v[Y::kLoads];
     auto address = [&](int u, const Pages& x) {
-        const int page = __builtin_amdgcn_readlane(x.page, wave);
-        const int in = (tl.at(u) * kBN + 16 * wave) & ((1 << a.ps_log2) - 1);
+        const int page = __builtin_amdgcn_readlane(x.page, wave * Y::kLoadRows / 16);
+        const int in = (tl.at(u) * kBN + Y::kLoadRows * wave) & ((1 << a.ps_log2) - 1);
         return a.kv + (int64_t)page * a.page_stride + head_off + (int64_t)in * Y::kRow + g_off;
     };
     auto load = [&](const char* base, u32x4 (&to)[Y::kLoads]) {
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 #pragma unroll
         for (int i = 0; i < Y::kLoads; ++i) {
             const int rr = i * Y::kRowsPerLoad + st_row;
-            *(u32x4*)(&s_kv[to][0][0] + (wave * 16 + rr) * Y::kRow + (st_ch ^ Y::fk(rr)) * 16) =
+            *(u32x4*)(&s_kv[to][0][0] + (wave * Y::kLoadRows + rr) * Y::kRow + (st_ch ^ Y::fk(wave * Y::kLoadRows + rr)) * 16) =
                 next_k[i];
         }
     };
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 #pragma unroll
         for (int i = 0; i < Y::kLoads; ++i) {
             const int rr = i * Y::kRowsPerLoad + st_row;
-            *(u32x4*)(&s_kv[to][1][0] + (wave * 16 + rr) * Y::kRow + (st_ch ^ Y::fv(rr)) * 16) =
+            *(u32x4*)(&s_kv[to][1][0] + (wave * Y::kLoadRows + rr) * Y::kRow + (st_ch ^ Y::fv(wave * Y::kLoadRows + rr)) * 16) =
                 next_v[i];
         }
     };
@@ -247,12 +252,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     // whether all tokens of a tile are visible to all rows from p to p_last
     auto plain_to = [&](int u, uint32_t ok4, int p, int p_last) {
         const int j0 = tl.at(u) * kBN;
-        return ok4 == 15u && j0 + kBN - 1 <= p &&
+        return ok4 == (1u << Y::kPages) - 1 && j0 + kBN - 1 <= p &&
                (!a.window || j0 > p_last - a.window || j0 + kBN <= a.sinks);
     };
 
     Pages now = check(0, look_up(0));
-    uint32_t ok4 = (uint32_t)__ballot(now.ok) & 15u;
+    uint32_t ok4 = (uint32_t)__ballot(now.ok) & ((1u << Y::kPages) - 1);
     if (tid < 2) s_fix[tid] = -1;
     __syncthreads();
     {
@@ -275,14 +280,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         const Pages here = now;
         const uint32_t ok_here = ok4;
         now = check(un, page_next);
-        ok4 = (uint32_t)__ballot(now.ok) & 15u;
+        ok4 = (uint32_t)__ballot(now.ok) & ((1u << Y::kPages) - 1);
         const char* from = address(un, now);
         load(from, next_k);
         page_next = look_up(min(u + 2, tl.n - 1));
 
-        f32x16 z[2];
+        f32x16 z[kBN / 32];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < kBN / 32; ++t) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) z[t][x] = 0.0f;
 #pragma unroll
@@ -298,11 +303,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             return ((ok_here >> ((j - j0) >> 4)) & 1) && j <= pos &&
                    (!a.window || j > pos - a.window || j < a.sinks);
         };
-        settle(z[0]);
-        settle(z[1]);
+#pragma unroll
+        for (int t = 0; t < kBN / 32; ++t) settle(z[t]);
         if (!plain_to(u, ok_here, w0, w1)) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kBN / 32; ++t)
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
                     if (!sees(j0 + 32 * t + 8 * (x / 4) + 4 * half + x % 4)) z[t][x] = -INFINITY;
@@ -310,9 +315,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 
         float top = z[0][0];
 #pragma unroll
-        for (int x = 1; x < 16; ++x) top = fmaxf(top, z[0][x]);
+        for (int t = 0; t < kBN / 32; ++t)
 #pragma unroll
-        for (int x = 0; x < 16; ++x) top = fmaxf(top, z[1][x]);
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, z[t][x]);
         top = pair_max(top) * c;
         // the reference may lag the maximum by 2^kLazy: the sums have the room
         // (fp32), and bf16's relative step is the same everywhere
@@ -325,9 +330,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             for (int i = 0; i < kOut; ++i) o[i] *= f;
         }
         const float ref = m == -INFINITY ? 0.0f : m;      // nothing seen yet: all p are 0
-        u32x4 p[4];                // 16 tokens each, as the second product takes them
+        u32x4 p[kBN / 16];                // 16 tokens each, as the second product takes them
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kBN / 32; ++t)
 #pragma unroll
             for (int x = 0; x < 16; x += 2) {
                 const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x], c, -ref));
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             }
         store_k((u + 1) & 1);
 #pragma unroll
-        for (int s4 = 0; s4 < 4; ++s4)
+        for (int s4 = 0; s4 < kBN / 16; ++s4)
 #pragma unroll
             for (int i = 0; i < kOut; ++i) {
                 const lds_t at = vb + v_base + s4 * 16 * Y::kRow + ((64 * i) ^ v_x);
@@ -379,7 +384,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     }
 #pragma unroll
     for (int i = 0; i < kOut; ++i) settle(o[i]);
-    if (err && lane < 4) report_error(a.err, err);
+    if (err && lane < Y::kPages) report_error(a.err, err);
 
     l = pair_sum(l);
     if (!live) return;
@@ -454,7 +459,8 @@ hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
 
 hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream) {
     if (head_dim == 64) return launch_tiles<64>(a, stream);
-    return launch_tiles<128>(a, stream);
+    if (head_dim == 128) return launch_tiles<128>(a, stream);
+    return launch_tiles<256>(a, stream);
 }
 
 }  // namespace star
