@@ -1,8 +1,8 @@
 """Plain restatement of the paged cache's operators -- TEST INFRASTRUCTURE.
 
 Page tables: one slot and one page after the other, in order.  Attention: one
-request, query head and row after the other over the request's tokens in a
-plain row, in 64 bits.  Host tensors in and out; nothing here imports the HIP
+request and row after the other over the request's tokens in a plain row, in
+64 bits.  Host tensors in and out; nothing here imports the HIP
 path.
 """
 from __future__ import annotations
@@ -174,17 +174,17 @@ def attend(q, k_new, v_new, kv, table, seq_len, q_start=None, *, scale, window=0
             if window:
                 see &= (j > p - window) | (j < sinks)
             jj = torch.nonzero(see).squeeze(1)
-            for h in range(Hq):
-                kh, vh = k[h // g][jj], v[h // g][jj]
-                qh = q[lo + i, h].double()
-                if jj.numel() == 0:
-                    continue
-                z = scale * (kh @ qh)
-                top = z.max()
-                e = torch.exp(z - top)
-                pr = e / e.sum()
-                out[lo + i, h] = (pr[:, None] * vh).sum(0)
-                mass[lo + i, h] = (pr[:, None] * vh.abs()).sum(0)
-                lse[lo + i, h] = top + torch.log(e.sum())
-                reach[lo + i, h] = (abs(scale) * (kh.abs() @ qh.abs())).max()
+            if jj.numel() == 0:
+                continue
+            # query head h reads key-value head h // g
+            kh, vh = (t[:, jj].repeat_interleave(g, dim=0) for t in (k, v))
+            qh = q[lo + i].double()[:, :, None]
+            z = scale * (kh @ qh)[:, :, 0]
+            top = z.max(dim=1).values
+            e = torch.exp(z - top[:, None])
+            pr = (e / e.sum(1, keepdim=True))[:, None]
+            out[lo + i] = (pr @ vh)[:, 0]
+            mass[lo + i] = (pr @ vh.abs())[:, 0]
+            lse[lo + i] = top + torch.log(e.sum(1))
+            reach[lo + i] = (abs(scale) * (kh.abs() @ qh.abs())[:, :, 0]).max(dim=1).values
     return dict(out=out, lse=lse, written=written, mass=mass, reach=reach, kv=kv_out, flags=flags)

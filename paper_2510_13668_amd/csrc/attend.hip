@@ -691,9 +691,7 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     static_assert(512 <= kMaxTickets, "one ticket per workgroup");
     pl.min_steps = 1;
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
-    const int64_t rows = (int64_t)p.n_rows * (p.n_heads / p.n_kv_heads);
-    pl.tiled = !decode && p.dtype == STAR_BF16 &&
-               rows >= 64 * (int64_t)p.n_seq;
+    if (!decode) plan_attend_tiles(p, pl);
     return pl;
 }
 
@@ -701,6 +699,7 @@ hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype
                          hipStream_t stream) {
     AttendArgs a = args;
     a.min_steps = pl.min_steps;
+    a.splits = pl.splits;
     if (a.n_seq == 0 || a.n_rows == 0) return hipSuccess;
     if (pl.tiled) return launch_attend_tiles(a, head_dim, stream);
     if (dtype == STAR_BF16) {

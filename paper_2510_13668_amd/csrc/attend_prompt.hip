@@ -1,6 +1,6 @@
 // Attention of many new tokens over the paged key-value cache: the bf16 kernel
 // of star_attend_prompt whose keys and values go through LDS.
-#include <type_traits>
+#include <algorithm>
 
 #include "attend.hpp"
 #include "star_common.hpp"
@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
 constexpr int kThreads = 256, kWaves = 4;
+constexpr int kPartTiles = 16;   // tiles that are worth a part of their own
 constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may lag
 
 typedef __attribute__((address_space(3))) char* lds_t;
@@ -46,6 +47,10 @@ __device__ inline float pair_sum(float v) {
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
+// floats a thread leaves in a part: its outputs, maximum and sum (padded)
+template <int D>
+constexpr int kPartFloats = D / 2 + 4;
+
 // ---------------------------------------------------------------------------
 // One workgroup: 128 (token, query head) rows of one request that share a
 // key-value head, tokens before heads, so that a group's heads share every
@@ -63,6 +68,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     __shared__ __attribute__((aligned(1024))) char s_kv[2][2][Y::kTile];
     __shared__ int64_t s_tmp[kWaves + 1];
     __shared__ int s_slot[2], s_fix[2];
+    __shared__ uint32_t s_ticket;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -70,7 +76,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 
     // which request and which of its blocks of rows: those with the longest
     // prefixes first, so that the launch ends on short ones
-    const int head = blockIdx.x % a.n_kv, nth = blockIdx.x / a.n_kv;
+    const int head = blockIdx.x % a.n_kv;
+    const int part = blockIdx.x / a.n_kv % a.splits, nth = blockIdx.x / a.n_kv / a.splits;
     int b, block;
     if (a.n_seq <= 64) {
         // one request a lane, every wave by itself: the largest last position X
@@ -161,6 +168,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
     const Tiles tl = tiles_of<kBN>(a, p0, p1);
+    // this workgroup's share of the tiles: all, or one of `parts`, which pay from
+    // about sixteen tiles each (512 rows after 16000 tokens: 416 -> 174 us; after
+    // 512, two parts of eight: 38 -> 43)
+    const int parts = max(1, min(a.splits, tl.n / kPartTiles));
+    if (part >= parts) return;
+    const int u0 = (int)((int64_t)tl.n * part / parts);
+    const int u1 = (int)((int64_t)tl.n * (part + 1) / parts);
     const int64_t v_off = (int64_t)a.n_kv * Y::kRow << a.ps_log2;
     const int64_t head_off = (int64_t)head * Y::kRow << a.ps_log2;
     int32_t err = 0;
@@ -256,34 +270,34 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
                (!a.window || j0 > p_last - a.window || j0 + kBN <= a.sinks);
     };
 
-    Pages now = check(0, look_up(0));
+    Pages now = check(u0, look_up(u0));
     uint32_t ok4 = (uint32_t)__ballot(now.ok) & ((1u << Y::kPages) - 1);
     if (tid < 2) s_fix[tid] = -1;
     __syncthreads();
     {
-        const char* from = address(0, now);
+        const char* from = address(u0, now);
         load(from, next_k);
         load(from + v_off, next_v);
-        store_k(0);
-        store_v(0, 0, plain_to(0, ok4, p0, p1));
+        store_k(u0 & 1);
+        store_v(u0 & 1, u0, plain_to(u0, ok4, p0, p1));
     }
-    int page_next = look_up(min(1, tl.n - 1));
+    int page_next = look_up(min(u0 + 1, u1 - 1));
     // the second wave of a SIMD goes first where both could: the two drift into
     // opposite phases, one's products beside the other's softmax
     if (__builtin_amdgcn_s_getreg(3 << 11 | 4) & 1) __builtin_amdgcn_s_setprio(1);
-    for (int u = 0; u < tl.n; ++u) {
+    for (int u = u0; u < u1; ++u) {
         __syncthreads();          // tile u is in its buffer, and the other one is done with
         const lds_t kb = (lds_t)&s_kv[u & 1][0][0], vb = (lds_t)&s_kv[u & 1][1][0];
         const int j0 = tl.at(u) * kBN;
         // (the last tile is loaded twice, so that no step hangs on a condition)
-        const int un = min(u + 1, tl.n - 1);
+        const int un = min(u + 1, u1 - 1);
         const Pages here = now;
         const uint32_t ok_here = ok4;
         now = check(un, page_next);
         ok4 = (uint32_t)__ballot(now.ok) & ((1u << Y::kPages) - 1);
         const char* from = address(un, now);
         load(from, next_k);
-        page_next = look_up(min(u + 2, tl.n - 1));
+        page_next = look_up(min(u + 2, u1 - 1));
 
         f32x16 z[kBN / 32];
 #pragma unroll
@@ -387,6 +401,49 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     if (err && lane < Y::kPages) report_error(a.err, err);
 
     l = pair_sum(l);
+    if (parts > 1) {
+        // The parts meet in the workspace, lane by lane as they are; the last to
+        // arrive joins all in order
+        constexpr uint32_t kPlane = kThreads * 16;               // 16 bytes a thread
+        constexpr uint32_t kBytes = kPartFloats<D> * kThreads * 4;
+        const uint32_t id = (uint32_t)(nth * a.n_kv + head);
+        const __amdgpu_buffer_rsrc_t ws =
+            xch_rsrc(a.part + (size_t)id * a.splits * kBytes, (uint32_t)parts * kBytes);
+        const uint32_t mine = (uint32_t)part * kBytes + tid * 16;
+        xch_store(u32x4{__float_as_uint(m), __float_as_uint(l), 0, 0}, ws, mine);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4)
+                xch_store(u32x4{__float_as_uint(o[i][x]), __float_as_uint(o[i][x + 1]),
+                                __float_as_uint(o[i][x + 2]), __float_as_uint(o[i][x + 3])},
+                          ws, mine + (1 + 4 * i + x / 4) * kPlane);
+        xch_wait_stores();
+        if (!xch_last_arrival(a.tickets + id, (uint32_t)parts, &s_ticket)) return;
+        m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[i][x] = 0.0f;
+        for (int w = 0; w < parts; ++w) {
+            const uint32_t at = (uint32_t)w * kBytes + tid * 16;
+            const u32x4 ml = xch_load(ws, at);
+            u32x4 v[4 * kOut];
+#pragma unroll
+            for (int i = 0; i < 4 * kOut; ++i) v[i] = xch_load(ws, at + (1 + i) * kPlane);
+            const float peak = fmaxf(m, __uint_as_float(ml[0]));
+            const float ref = peak == -INFINITY ? 0.0f : peak;
+            const float f0 = __builtin_amdgcn_exp2f(m - ref);
+            const float f1 = __builtin_amdgcn_exp2f(__uint_as_float(ml[0]) - ref);
+            m = peak;
+            l = l * f0 + __uint_as_float(ml[1]) * f1;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    o[i][x] = o[i][x] * f0 + __uint_as_float(v[4 * i + x / 4][x & 3]) * f1;
+        }
+    }
     if (!live) return;
     const int64_t at = q_row * a.n_heads + q_head;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // a row that sees nothing is 0
@@ -405,11 +462,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 }
 
 // ---------------------------------------------------------------------------
-// The new tokens of prompts into their pages: one workgroup per token, 16
-// bytes a thread.
+// The new tokens of prompts into their pages, sixteen rows a workgroup: a lane
+// each finds their places, then all copy, 16 bytes a thread and several in
+// flight (a token a workgroup waited out the same chain 16 times: 18 us for
+// 12700 tokens of 2 KB, now 10).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes) {
-    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    constexpr int kStoreRows = 16;
+    __shared__ int64_t s_to[kStoreRows];
+    const int64_t row0 = (int64_t)blockIdx.x * kStoreRows;
+    if (threadIdx.x < kStoreRows) {
+        const int64_t row = row0 + threadIdx.x;
+        int64_t to = -1;
         // the request whose rows hold this one: the last that starts at or before it
         int lo = 0, hi = a.n_seq;
         while (lo < hi) {
@@ -418,36 +482,44 @@ __global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, in
             else hi = mid;
         }
         const int b = lo - 1;
-        if (b < 0) continue;
-        const int from = a.q_start[b], to = a.q_start[b + 1], L = a.seq_len[b];
-        if (from < 0 || row >= to || to > a.n_rows || L < 0 || L > a.max_pages << a.ps_log2 ||
-            to - from > L)
-            continue;
-        const int j = (int)(L - (to - from) + (row - from));
-        const int page = a.table[(int64_t)b * a.max_pages + (j >> a.ps_log2)];
-        if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-        const int in = j & ((1 << a.ps_log2) - 1);
-        const int all = a.n_kv * row_bytes;               // bytes of one token's keys
-        char* base = a.kv + (int64_t)page * a.page_stride;
-        for (int x = threadIdx.x * 16; x < 2 * all; x += kThreads * 16) {
-            const int y = x < all ? x : x - all;
-            const int head = y / row_bytes, d = y - head * row_bytes;
-            const char* src = (x < all ? a.kn : a.vn) + row * a.kv_stride + y;
-            char* dst = base + ((int64_t)((x < all ? 0 : a.n_kv) + head) << a.ps_log2) * row_bytes +
-                        (int64_t)in * row_bytes + d;
-            *(u32x4*)dst = *(const u32x4*)src;
+        if (b >= 0 && row < a.n_rows) {
+            const int from = a.q_start[b], end = a.q_start[b + 1], L = a.seq_len[b];
+            if (from >= 0 && row < end && end <= a.n_rows && L >= 0 &&
+                L <= a.max_pages << a.ps_log2 && end - from <= L) {
+                const int j = (int)(L - (end - from) + (row - from));
+                const int page = a.table[(int64_t)b * a.max_pages + (j >> a.ps_log2)];
+                if ((uint32_t)page < (uint32_t)a.n_pages)
+                    to = (int64_t)page * a.page_stride +
+                         (int64_t)(j & ((1 << a.ps_log2) - 1)) * row_bytes;
+            }
         }
+        s_to[threadIdx.x] = to;
+    }
+    __syncthreads();
+    const int pieces = a.n_kv * row_bytes / 16;            // of one token's keys
+    const int per = row_bytes / 16;                        // of one head's: 8, 16 or 32
+    for (int x = threadIdx.x; x < kStoreRows * 2 * pieces; x += kThreads) {
+        const int i = x / (2 * pieces), y = x - i * 2 * pieces;
+        const bool value = y >= pieces;
+        const int z = value ? y - pieces : y, head = z / per, d = (z - head * per) * 16;
+        const int64_t to = s_to[i];
+        if (to < 0) continue;
+        const u32x4 v = *(const u32x4*)((value ? a.vn : a.kn) + (row0 + i) * a.kv_stride +
+                                        (int64_t)z * 16);
+        *(u32x4*)(a.kv + to + ((int64_t)((value ? a.n_kv : 0) + head) << a.ps_log2) * row_bytes +
+                  d) = v;
     }
 }
 
+// an upper bound: every request has one block at most that is not full
+int64_t tile_blocks(int64_t n_rows, int g, int n_seq) { return n_rows * g / kBM + n_seq; }
+
 template <int D>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
-    // blocks of rows: every request has one that is not full at most
-    const int64_t blocks = (int64_t)a.n_rows * a.g / kBM + a.n_seq;
-    const int64_t grid = blocks * a.n_kv;
+    const int64_t grid = tile_blocks(a.n_rows, a.g, a.n_seq) * a.n_kv * a.splits;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(store_tokens_kernel, dim3(a.n_rows < 4096 ? a.n_rows : 4096),
-                       dim3(kThreads), 0, stream, a, 2 * D);
+    hipLaunchKernelGGL(store_tokens_kernel, dim3((a.n_rows + 15) / 16), dim3(kThreads), 0, stream, a,
+                       2 * D);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_tiles_kernel<D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
@@ -456,6 +528,29 @@ hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
+    const int g = p.n_heads / p.n_kv_heads;
+    const int64_t rows = (int64_t)p.n_rows * g;
+    // workgroups, if the requests' last blocks are half full
+    const int64_t groups = (rows + (int64_t)p.n_seq * kBM / 2) / kBM * p.n_kv_heads;
+    pl.tiled = p.dtype == STAR_BF16 && groups >= 112;
+    // Two fit a CU; launches that leave places free cut the keys
+    pl.splits = 1;
+    const int64_t most = tile_blocks(p.n_rows, g, p.n_seq) * p.n_kv_heads;
+    if (pl.tiled && groups <= 256 && most <= kMaxTickets) {
+        // (no more than the longest request the page table holds could use:
+        // workgroups that find nothing to do crowd the others' CUs, 38 -> 45 us
+        // for 512 rows after 512 tokens)
+        const int tile = p.head_dim == 256 ? Lay<256>::kBN : Lay<128>::kBN;
+        const int64_t longest = (int64_t)p.max_pages * p.page_size / tile / kPartTiles;
+        pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / groups, longest));
+    }
+    if (pl.tiled)
+        pl.part_bytes = pl.splits == 1 ? 0
+                                       : (size_t)most * pl.splits * (p.head_dim / 2 + 4) *
+                                             kThreads * sizeof(float);
+}
 
 hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream) {
     if (head_dim == 64) return launch_tiles<64>(a, stream);

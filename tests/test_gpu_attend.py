@@ -216,6 +216,76 @@ def test_prompt(lens, new, Hq, Hkv, D, dtype):
     check(c, False, window=29, sinks=3)
 
 
+# Enough key-value heads put small prompts on the tiled kernel, which takes
+# bf16 calls of 112 workgroups (128 rows of one head each) and more.
+WIDE = 112
+
+
+def tiled(c):
+    """The call is the tiled kernel's: no workspace but the parts of cut blocks."""
+    size = star.attend_prompt_workspace_size(c.params(0, 0)) - star.STAR_WS_HEADER_BYTES
+    return size % (4096 * (c.D // 8 + 1)) == 0
+
+
+@pytest.mark.parametrize("lens,new", [([1], [64]), ([17, 64, 5], [17, 30, 1]), ([100], [100]),
+                                      ([200, 0, 16, 80], [130, 0, 16, 33]), ([260], [129])])
+@pytest.mark.parametrize("g,D", [(1, 64), (2, 128), (1, 256)])
+def test_prompt_tiled(lens, new, g, D):
+    lens = [max(a, b) for a, b in zip(lens, new)]
+    c = Cache(sum(lens), lens, new, WIDE * g, WIDE, D, ps=16 if D < 256 else 32, peak=2.0)
+    assert tiled(c)
+    check(c, False)
+    check(c, False, window=29, sinks=3)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (64, 0), (70, 70), (64, 1),
+                                          (2 ** 31 - 1, 3), (50, 2 ** 31 - 1), (100, 33)])
+def test_prompt_tiled_windows(window, sinks):
+    c = Cache(7, [190, 160], [100, 31], WIDE, WIDE, 64)
+    c.scale = -0.2                                     # and the least products first
+    assert tiled(c)
+    check(c, False, window, sinks)
+
+
+def test_prompt_tiled_infinities_and_bad_contents():
+    c = Cache(4, [150, 40, 90], [70, 5, 33], WIDE, WIDE, 64)
+    c.scale = 0.05
+    assert tiled(c)
+    q, k, v = c.split(c.qkv)
+    inf, nan = math.inf, math.nan
+    v[40, 0, 9], v[41, 1, 3], v[60, 0, 11], v[69, 5, 63] = inf, nan, -inf, inf
+    k[55, 1, :] = nan
+    v[75 + 20, 1, 2] = inf
+    page = int(c.table[0, 1])
+    c.kv[page, 1, 2, 3, 30], c.kv[page, 0, 3, 3, 30] = nan, nan         # token 19
+    check(c, False)
+    check(c, False, window=25, sinks=2)
+    check(c, False, window=25, sinks=20)
+    c.len[1] = 4                                       # more new tokens than tokens
+    c.table[2, 1], c.table[0, 6] = -1, 10 ** 6         # cached tokens and new ones
+    check(c, False, flags=star.DEV_BAD_LEN | star.DEV_BAD_PAGE)
+    check(c, False, window=25, sinks=2, flags=star.DEV_BAD_LEN | star.DEV_BAD_PAGE)
+
+
+def test_prompt_tiled_many_requests():
+    new = [1 + 37 * b % 40 for b in range(70)]
+    c = Cache(5, [n + b % 3 * 20 for b, n in enumerate(new)], new, 32, 16, 64)
+    assert tiled(c)
+    check(c, False)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T,past,window,sinks", [
+    (16, 16, 64, 900, 2000, 0, 0), (32, 16, 128, 450, 1700, 0, 0), (32, 16, 128, 450, 1900, 1700, 9),
+    (28, 28, 256, 490, 700, 0, 0)])
+def test_prompt_tiled_cut_keys(Hq, Hkv, D, T, past, window, sinks):
+    """Few blocks over long caches: several workgroups share a block's keys."""
+    c = Cache(6, [past + T], [T], Hq, Hkv, D, ps=64, peak=3.0)
+    assert tiled(c) and star.attend_prompt_workspace_size(c.params(0, 0)) > 1 << 20
+    a = check(c, False, window, sinks)
+    b = run(c, False, window, sinks)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])   # no order of arrival in it
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (64, 0), (100, 70), (128, 1),
                                           (2 ** 31 - 1, 3), (500, 2 ** 31 - 1)])
 def test_prompt_windows(window, sinks):
