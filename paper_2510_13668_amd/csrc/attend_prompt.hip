@@ -462,16 +462,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 }
 
 // ---------------------------------------------------------------------------
-// The new tokens of prompts into their pages, sixteen rows a workgroup: a lane
-// each finds their places, then all copy, 16 bytes a thread and several in
-// flight (a token a workgroup waited out the same chain 16 times: 18 us for
-// 12700 tokens of 2 KB, now 10).
+// The new tokens of prompts into their pages, `rows` (at most 4) tokens a workgroup:
+// a lane each finds their places, then all copy, 16 bytes a thread and several in
+// flight.  Long calls take four (18 -> 13 us for 12700 tokens of 2 KB), whose
+// places are looked up at once; short ones one, which starts sooner.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes) {
-    constexpr int kStoreRows = 16;
-    __shared__ int64_t s_to[kStoreRows];
-    const int64_t row0 = (int64_t)blockIdx.x * kStoreRows;
-    if (threadIdx.x < kStoreRows) {
+__global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, int row_bytes,
+                                                                int rows) {
+    __shared__ int64_t s_to[4];
+    const int64_t row0 = (int64_t)blockIdx.x * rows;
+    if ((int)threadIdx.x < rows) {
         const int64_t row = row0 + threadIdx.x;
         int64_t to = -1;
         // the request whose rows hold this one: the last that starts at or before it
@@ -498,16 +498,26 @@ __global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, in
     __syncthreads();
     const int pieces = a.n_kv * row_bytes / 16;            // of one token's keys
     const int per = row_bytes / 16;                        // of one head's: 8, 16 or 32
-    for (int x = threadIdx.x; x < kStoreRows * 2 * pieces; x += kThreads) {
-        const int i = x / (2 * pieces), y = x - i * 2 * pieces;
-        const bool value = y >= pieces;
-        const int z = value ? y - pieces : y, head = z / per, d = (z - head * per) * 16;
-        const int64_t to = s_to[i];
-        if (to < 0) continue;
-        const u32x4 v = *(const u32x4*)((value ? a.vn : a.kn) + (row0 + i) * a.kv_stride +
-                                        (int64_t)z * 16);
-        *(u32x4*)(a.kv + to + ((int64_t)((value ? a.n_kv : 0) + head) << a.ps_log2) * row_bytes +
-                  d) = v;
+    constexpr int kUnroll = 4;
+    for (int x0 = threadIdx.x; x0 < rows * 2 * pieces; x0 += kUnroll * kThreads) {
+        u32x4 v[kUnroll];
+        char* to[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int x = x0 + u * kThreads, i = x / (2 * pieces), y = x - i * 2 * pieces;
+            const bool value = y >= pieces;
+            const int z = value ? y - pieces : y, head = z / per, d = (z - head * per) * 16;
+            to[u] = nullptr;
+            if (i < rows && s_to[i] >= 0) {
+                v[u] = *(const u32x4*)((value ? a.vn : a.kn) + (row0 + i) * a.kv_stride +
+                                       (int64_t)z * 16);
+                to[u] = a.kv + s_to[i] +
+                        ((int64_t)((value ? a.n_kv : 0) + head) << a.ps_log2) * row_bytes + d;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (to[u]) *(u32x4*)to[u] = v[u];
     }
 }
 
@@ -518,8 +528,9 @@ template <int D>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
     const int64_t grid = tile_blocks(a.n_rows, a.g, a.n_seq) * a.n_kv * a.splits;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(store_tokens_kernel, dim3((a.n_rows + 15) / 16), dim3(kThreads), 0, stream, a,
-                       2 * D);
+    const int store = a.n_rows > 4096 ? 4 : 1;
+    hipLaunchKernelGGL(store_tokens_kernel, dim3((a.n_rows + store - 1) / store), dim3(kThreads),
+                       0, stream, a, 2 * D, store);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attend_tiles_kernel<D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
