@@ -1,7 +1,9 @@
 /*
  * libstar -- MI355X (gfx950) hot path of STAR's decode-phase rescheduler
  * (arXiv 2510.13668): remaining-length prediction, load projection and
- * migration-candidate scoring for one rescheduling round.
+ * migration-candidate scoring for one rescheduling round, and between rounds
+ * the decode instances' paged key-value cache: page tables that follow the
+ * plan, and attention over them.
  *
  * Vocabulary (Section 5.2, problem formulation):
  *   instances I = {0..n_inst-1}; request r sits on instance inst_of[r]
@@ -438,7 +440,8 @@ typedef struct {
  * the migrations of a plan in one call, all as of the state on entry.
  *   Slot b afterwards holds new_len[b] tokens on instance inst_of[b] (its own
  * instance if inst_of is NULL; star_plan_migrations leaves the planned
- * placement in the same form).  Its first keep = min(new_len[b], seq_len[a])
+ * placement in the same form, in an array apart from seq_inst, which says where
+ * the pages are).  Its first keep = min(new_len[b], seq_len[a])
  * tokens are those of slot a = parent[b] (b itself if parent is NULL; -1:
  * none, keep = 0).  Of their pages,
  *   - on the same instance the full ones become shared with a (each further
@@ -494,8 +497,9 @@ star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
  *     window == 0  or  j > p - window  or  j < sinks,
  * and gives
  *     out = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j exp(scale q . k_j)
- * (natural logarithm; 0 and -infinity where nothing is visible).  What a row
- * does not see does not change it, whatever it holds; pages that no row sees
+ * (natural logarithm; 0 and -infinity where nothing is visible, or every
+ * visible score is -infinity).  What a row does not see does not change it,
+ * whatever it holds; pages that no row sees
  * are not read, and their table entries mean nothing.
  *   Both calls first store the new tokens: k_new and v_new are the keys and
  * values of the last tokens of each request, which seq_len counts already
@@ -542,7 +546,8 @@ star_status star_attend_decode(const star_attend_params* p, const void* q, const
 /* Several new tokens a request: q_start int32 [n_seq + 1] (ascending, at most
  * n_rows) gives slot b rows q_start[b] .. q_start[b + 1] - 1 of q, k_new,
  * v_new, out and lse; they are its last tokens, in order, and no more than
- * seq_len[b].  Rows outside every range are left as they were. */
+ * seq_len[b].  Rows outside every range are left as they were.  Where q_start
+ * falls, requests behind the fall may be left out beside those it names. */
 size_t star_attend_prompt_workspace_size(const star_attend_params* p);
 
 star_status star_attend_prompt(const star_attend_params* p, const void* q, const void* k_new,

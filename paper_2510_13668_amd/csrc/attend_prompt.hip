@@ -153,8 +153,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int q_head = head * a.g + row % a.g;
 
     // a negative scale turns the queries' signs, so that the largest score is
-    // the largest product
-    const float c = fabsf(a.scale_log2);
+    // the largest product; a scale of 0 is the least number, so that hidden keys'
+    // -infinity stays what it is
+    const float c = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
     const uint32_t turn = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
     u32x4 q[kSteps];
     {
@@ -217,7 +218,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 #pragma unroll
         for (int i = 0; i < Y::kLoads; ++i) {
             const int rr = i * Y::kRowsPerLoad + st_row;
-            *(u32x4*)(&s_kv[to][0][0] + (wave * Y::kLoadRows + rr) * Y::kRow + (st_ch ^ Y::fk(wave * Y::kLoadRows + rr)) * 16) =
+            const int in_tile = wave * Y::kLoadRows + rr;
+            *(u32x4*)(&s_kv[to][0][0] + in_tile * Y::kRow + (st_ch ^ Y::fk(in_tile)) * 16) =
                 next_k[i];
         }
     };
@@ -243,7 +245,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 #pragma unroll
         for (int i = 0; i < Y::kLoads; ++i) {
             const int rr = i * Y::kRowsPerLoad + st_row;
-            *(u32x4*)(&s_kv[to][1][0] + (wave * Y::kLoadRows + rr) * Y::kRow + (st_ch ^ Y::fv(wave * Y::kLoadRows + rr)) * 16) =
+            const int in_tile = wave * Y::kLoadRows + rr;
+            *(u32x4*)(&s_kv[to][1][0] + in_tile * Y::kRow + (st_ch ^ Y::fv(in_tile)) * 16) =
                 next_v[i];
         }
     };

@@ -194,6 +194,13 @@ def _ptr(t: Optional[torch.Tensor]):
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+def _same_device(t: torch.Tensor, stream):
+    """The tensor's device is the current one, and the stream's."""
+    dev = t.get_device()
+    if dev != torch.cuda.current_device() or (stream is not None and stream.device_index != dev):
+        raise ValueError("the tensors' device has to be the current one and the stream's")
+
+
 def _stream(stream) -> int:
     """The hipStream_t of `stream`, or of the current device's current stream."""
     if stream is None:
@@ -421,6 +428,7 @@ def assign_pages(p: PagesParams, parent, new_len, inst_of, table, seq_len, seq_i
     instance.  parent, inst_of: None for none; seq_inst, seq_inst_out may be
     None where p.n_inst is 1.  Outputs may be their inputs (table_out only
     without parents)."""
+    _same_device(kv, stream)
     _check("star_assign_pages", lib().star_assign_pages(
         ctypes.byref(p), *_ptrs(parent, new_len, inst_of, table, seq_len, seq_inst, refs,
                                 kv, table_out, seq_len_out, seq_inst_out, refs_out),
@@ -434,6 +442,7 @@ def compact_pages_workspace_size(p: PagesParams) -> int:
 def compact_pages(p: PagesParams, table, seq_len, refs, kv, table_out, refs_out, n_live,
                   ws: Workspace, stream=None):
     """star_compact_pages: every instance's live pages to its lowest indices."""
+    _same_device(kv, stream)
     _check("star_compact_pages", lib().star_compact_pages(
         ctypes.byref(p), *_ptrs(table, seq_len, refs, kv, table_out, refs_out, n_live),
         ws.ptr, ws.nbytes, _stream(stream)))
@@ -491,6 +500,7 @@ def attend_decode(p: AttendParams, q, k_new, v_new, kv, table, seq_len, out, lse
     heads, head_dim], rows p.q_stride and p.kv_stride elements apart (columns
     of one projection's output do); kv: one layer of the pool, [n_pages, 2,
     n_kv_heads, page_size, head_dim]; lse: None for none."""
+    _same_device(kv, stream)
     _check("star_attend_decode", lib().star_attend_decode(
         ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
         *_ptrs(table, seq_len, out, lse), ws.ptr, ws.nbytes, _stream(stream)))
@@ -505,6 +515,7 @@ def attend_prompt(p: AttendParams, q, k_new, v_new, kv, table, seq_len, q_start,
     """star_attend_prompt: several new tokens a slot, rows q_start[b] ..
     q_start[b + 1] - 1 of q, k_new, v_new, out and lse; otherwise as
     attend_decode."""
+    _same_device(kv, stream)
     _check("star_attend_prompt", lib().star_attend_prompt(
         ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
         *_ptrs(table, seq_len, q_start, out, lse), ws.ptr, ws.nbytes, _stream(stream)))

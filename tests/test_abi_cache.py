@@ -154,6 +154,22 @@ def test_binding_checks_the_tensors():
     star._strided(one, torch.bfloat16, (1, 8, 128), (5, 128, 1))
 
 
+def test_binding_refuses_another_device(monkeypatch):
+    class On:
+        def __init__(self, device):
+            self.device_index = device
+
+        def get_device(self):
+            return self.device_index
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    star._same_device(On(1), None)
+    star._same_device(On(1), On(1))
+    for tensor, stream in ((On(0), None), (On(1), On(0)), (On(0), On(0))):
+        with pytest.raises(ValueError):
+            star._same_device(tensor, stream)
+
+
 class _Meta:
     """A host tensor that says it is on a GPU."""
 
@@ -162,3 +178,9 @@ class _Meta:
 
     def __getattr__(self, name):
         return getattr(self.t, name)
+
+
+def test_attention_of_nothing_launches_nothing(L):
+    assert _decode(L, _attend(n_seq=0, n_rows=0)) == 0
+    assert _prompt(L, _attend(n_seq=0, n_rows=0)) == 0
+    assert _prompt(L, _attend(n_seq=4, n_rows=0)) == 0

@@ -247,6 +247,80 @@ def test_prompt_tiled_windows(window, sinks):
     check(c, False, window, sinks)
 
 
+@pytest.mark.parametrize("ps", [128, 256])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 0.3])
+def test_large_pages_and_scales(ps, scale):
+    lens = [1, 127, 128, 129, 400, 513]
+    for c, decode in ((Cache(18, lens, [1] * 6, 6, 2, 64, ps=ps), True),
+                      (Cache(19, lens, [1, 100, 1, 129, 30, 64], 4, 2, 128, ps=ps), False),
+                      (Cache(20, lens, [1, 20, 1, 9, 30, 64], WIDE, WIDE, 64, ps=ps), False)):
+        c.scale = scale
+        check(c, decode)
+        check(c, decode, window=70, sinks=3)
+
+
+def test_tiled_pages_out_of_the_window_may_be_gone():
+    c = Cache(21, [300, 150], [60, 40], WIDE, WIDE, 64)
+    assert tiled(c)
+    keep = run(c, False, window=40, sinks=20)
+    c.table[0, 2:12], c.table[1, 2:4] = -1, 10 ** 6      # tokens 32..191 and 32..63
+    out, lse, _, err = run(c, False, window=40, sinks=20)
+    assert err == 0 and torch.equal(out, keep[0]) and torch.equal(lse, keep[1])
+
+
+def test_very_many_requests():
+    """More requests than threads, waves and lanes hold one each, short ones
+    and some long ones: values that are the same for all of a request's tokens
+    come back whatever the weights."""
+    n, rng = 20000, np.random.default_rng(22)
+    lens = rng.integers(0, 3, n)
+    lens[rng.integers(0, n, 40)] = rng.integers(100, 400, 40)
+    used = -(-lens // 16)
+    M, pages = int(used.max()), int(used.sum())
+    j = np.arange(M)[None]
+    table = np.where(j < used[:, None], (np.cumsum(used) - used)[:, None] + j, -1)
+    value = torch.randint(-99, 100, (n,)).float()
+    owner = torch.from_numpy(np.repeat(np.arange(n), used))
+    kv = torch.randn((pages, 2, 1, 16, 64))
+    kv[:, 1] = value[owner][:, None, None, None]
+    for dtype in ("bf16", "f32"):
+        dt, code = TYPES[dtype]
+        p = star.attend_params(n, n, 2, 1, 64, code, 16, pages, M, 0.1)
+        dev = lambda t: t.to(DEV)
+        v_new = value[:, None, None].expand(n, 1, 64).to(dt).contiguous()
+        out = torch.full((n, 2, 64), 77.0, dtype=dt, device=DEV)
+        ws = star.Workspace(star.attend_decode_workspace_size(p))
+        print("many", dtype, flush=True)
+        star.attend_decode(p, dev(torch.randn((n, 2, 64)).to(dt)),
+                           dev(torch.randn((n, 1, 64)).to(dt)), dev(v_new), dev(kv.to(dt)),
+                           dev(torch.from_numpy(table.astype(np.int32))),
+                           dev(torch.from_numpy(lens.astype(np.int32))), out, None, ws)
+        want = torch.where(torch.from_numpy(lens) > 0, value, torch.zeros(()))
+        # sums of up to 400 probabilities over their own sum (bf16 pairs: 2^-16)
+        tol = 99 * (2.0 ** -8 + 2.0 ** -16 if dtype == "bf16" else 500 * U)
+        assert (out.cpu().double() - want[:, None, None]).abs().max() <= tol
+        assert ws.read_device_error() == 0
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    a = Cache(23, [2000, 40], [1, 1], 8, 2, 64)
+    b = Cache(24, [300, 200], [250, 90], 8, 2, 64)
+    want = run(a, True)[0], run(b, False)[0]
+    pa, pb = a.params(0, 0), b.params(0, 0)
+    wa = star.Workspace(star.attend_decode_workspace_size(pa))
+    wb = star.Workspace(star.attend_prompt_workspace_size(pb))
+    xa, xb, ka, kb = (t.to(DEV) for t in (a.qkv, b.qkv, a.kv, b.kv))
+    ta, la, tb, lb, sb = (t.to(DEV) for t in (a.table, a.len, b.table, b.len, b.start))
+    oa, ob = torch.empty_like(want[0], device=DEV), torch.empty_like(want[1], device=DEV)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        star.attend_decode(pa, *a.split(xa), ka, ta, la, oa, None, wa, s1)
+        star.attend_prompt(pb, *b.split(xb), kb, tb, lb, sb, ob, None, wb, s2)
+    torch.cuda.synchronize()
+    assert torch.equal(oa.cpu(), want[0]) and torch.equal(ob.cpu(), want[1])
+
+
 def test_prompt_tiled_infinities_and_bad_contents():
     c = Cache(4, [150, 40, 90], [70, 5, 33], WIDE, WIDE, 64)
     c.scale = 0.05
