@@ -163,18 +163,6 @@ __device__ inline float value_at(const uint32_t* w, int i) {
     return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
 
-// n outputs of one row
-template <int kDtype, int n>
-__device__ inline void store_out(char* to, const float* y) {
-#pragma unroll
-    for (int i = 0; i < n; i += 4) {
-        if constexpr (kDtype == STAR_BF16)
-            *(u32x2*)(to + 2 * i) =
-                u32x2{pack_bf16x2_rne(y[i], y[i + 1]), pack_bf16x2_rne(y[i + 2], y[i + 3])};
-        else
-            *(f32x4*)(to + 4 * i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
-    }
-}
 // a / b of two counts: 64-bit divisions, a hundred instructions and more each,
 // only where the counts need them
 __device__ inline int64_t quotient(int64_t a, int64_t b) {
@@ -701,7 +689,7 @@ hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype
     a.min_steps = pl.min_steps;
     a.splits = pl.splits;
     if (a.n_seq == 0 || a.n_rows == 0) return hipSuccess;
-    if (pl.tiled) return launch_attend_tiles(a, head_dim, stream);
+    if (pl.tiled) return launch_attend_tiles(a, dtype, head_dim, stream);
     if (dtype == STAR_BF16) {
         if (head_dim == 64) return launch_rows<STAR_BF16, 64>(a, pl.grid, stream);
         if (head_dim == 128) return launch_rows<STAR_BF16, 128>(a, pl.grid, stream);

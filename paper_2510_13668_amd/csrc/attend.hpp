@@ -98,5 +98,17 @@ __device__ inline uint32_t finite_part(uint32_t w) {
     const uint32_t hi = (w & 0x7F800000u) == 0x7F800000u ? 0u : w & 0xFFFF0000u;
     return lo | hi;
 }
+// n outputs of one row
+template <int kDtype, int n>
+__device__ inline void store_out(char* to, const float* y) {
+#pragma unroll
+    for (int i = 0; i < n; i += 4) {
+        if constexpr (kDtype == STAR_BF16)
+            *(u32x2*)(to + 2 * i) =
+                u32x2{pack_bf16x2_rne(y[i], y[i + 1]), pack_bf16x2_rne(y[i + 2], y[i + 3])};
+        else
+            *(f32x4*)(to + 4 * i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    }
+}
 
 }  // namespace star

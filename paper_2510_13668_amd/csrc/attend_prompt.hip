@@ -1,5 +1,5 @@
-// Attention of many new tokens over the paged key-value cache: the bf16 kernel
-// of star_attend_prompt whose keys and values go through LDS.
+// Attention of many new tokens over the paged key-value cache: the kernel of
+// star_attend_prompt whose keys and values go through LDS.
 #include <algorithm>
 
 #include "attend.hpp"
@@ -18,23 +18,28 @@ constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may 
 typedef __attribute__((address_space(3))) char* lds_t;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-template <int D>
+template <int kDtype, int D>
 struct Lay {
-    // tokens of a tile, a quarter a wave to load (256 wide, the registers hold
-    // 32 tokens' scores beside the output)
-    static constexpr int kBN = D == 256 ? 32 : 64;
+    static constexpr int kBytes = kDtype == STAR_BF16 ? 2 : 4;
+    static constexpr int kRow = kBytes * D;       // bytes of a token's keys (or values)
+    // tokens of a tile, a quarter a wave to load (two workgroups' tiles fit LDS;
+    // where a row fills the registers, one workgroup's do)
+    static constexpr int kBN = kRow > 256 ? 32 : 64;
     static constexpr int kPages = kBN / 16;       // sixteens of tokens, each in one page
     static constexpr int kLoadRows = kBN / 4;     // tokens that a wave loads
-    static constexpr int kRow = 2 * D;            // bytes of a token's keys (or values)
     static constexpr int kChunks = kRow / 16;     // 16-byte chunks of a row
     static constexpr int kTile = kBN * kRow;      // bytes of a tile's keys
     static constexpr int kRowsPerLoad = 1024 / kRow;
     static constexpr int kLoads = kLoadRows / kRowsPerLoad;   // 1 KiB loads of those
     // Chunk c of row r lies at chunk c ^ f(r) of the row.  Keys: 16 lanes read
-    // one chunk of 16 rows; values: 32 lanes read 32 bytes of 4 rows and the 32
-    // bytes beside; either way every bank is read once.
-    __device__ static int fk(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
-    __device__ static int fv(int r) { return D == 64 ? ((r >> 1) & 1) * 4 : (r & 3) * 4; }
+    // one chunk of 16 rows; bf16 values: 32 lanes read 32 bytes of 4 rows and the
+    // 32 bytes beside; fp32 values: 32 lanes 128 bytes of a row, the others of the
+    // fourth row on; in each case every bank is read once.
+    __device__ static int fk(int r) { return kRow == 128 ? (r >> 1) & 7 : r & 15; }
+    __device__ static int fv(int r) {
+        if (kDtype == STAR_F32) return ((r >> 2) & 1) * 8;
+        return kRow == 128 ? ((r >> 1) & 1) * 4 : (r & 3) * 4;
+    }
 };
 
 // the maximum of lanes l and l ^ 32
@@ -59,10 +64,11 @@ constexpr int kPartFloats = D / 2 + 4;
 // operand of O^T [d x rows] = V^T P^T, and the softmax needs one exchange with
 // lane l ^ 32 a tile.  V's fragments are read from LDS transposed.
 // ---------------------------------------------------------------------------
-template <int D>
+template <int kDtype, int D>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kernel(AttendArgs a) {
-    using Y = Lay<D>;
-    constexpr int kSteps = D / 16;       // contraction steps of a score
+    using Y = Lay<kDtype, D>;
+    constexpr bool kBf16 = kDtype == STAR_BF16;
+    constexpr int kSteps = Y::kRow / 32; // 32-byte steps of a score's contraction
     constexpr int kOut = D / 32;         // 32-wide blocks of the output
     constexpr int kBN = Y::kBN;
     __shared__ __attribute__((aligned(1024))) char s_kv[2][2][Y::kTile];
@@ -156,7 +162,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     // the largest product; a scale of 0 is the least number, so that hidden keys'
     // -infinity stays what it is
     const float c = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
-    const uint32_t turn = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    const uint32_t turn = a.scale_log2 < 0.0f ? (kBf16 ? 0x80008000u : 0x80000000u) : 0u;
     u32x4 q[kSteps];
     {
         const char* p = a.q + q_row * a.q_stride + (int64_t)q_head * Y::kRow + half * 16;
@@ -232,13 +238,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 #pragma unroll
             for (int i = 0; i < Y::kLoads; ++i)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) big = larger<STAR_BF16>(big, next_v[i][x]);
-            if (__any(not_finite<STAR_BF16>(big))) {
+                for (int x = 0; x < 4; ++x) big = larger<kDtype>(big, next_v[i][x]);
+            if (__any(not_finite<kDtype>(big))) {
 #pragma unroll
                 for (int i = 0; i < Y::kLoads; ++i)
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        next_v[i][x] = finite_part<STAR_BF16>(next_v[i][x]);
+                        next_v[i][x] = finite_part<kDtype>(next_v[i][x]);
                 s_fix[to] = u;
             }
         }
@@ -261,10 +267,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     // lane addresses of the fragments in a tile
     const int k_base = r32 * Y::kRow, k_x = (half ^ Y::fk(r32)) * 16;
     const int i16 = lane & 15;
-    const int v_base = (4 * half + (i16 >> 2)) * Y::kRow + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
-    const int v_x = Y::fv(i16 >> 2) * 16;
-    // (fv depends on a row's two lowest bits, D == 64: on its second; the
-    // fragments' first rows are multiples of four)
+    const int v_base = kBf16 ? (4 * half + (i16 >> 2)) * Y::kRow + ((lane >> 4) & 1) * 32 +
+                                   (i16 & 3) * 8
+                             : 4 * half * Y::kRow + r32 * 4;
+    // (fv depends on a row's bits below 8 alone, and the fragments' first rows are
+    // multiples of 8; a 32-wide block of the output is a whole number of its steps)
+    const int v_x = (kBf16 ? Y::fv(i16 >> 2) : 8 * half) * 16;
 
     // whether all tokens of a tile are visible to all rows from p to p_last
     auto plain_to = [&](int u, uint32_t ok4, int p, int p_last) {
@@ -309,10 +317,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             for (int x = 0; x < 16; ++x) z[t][x] = 0.0f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const bf16x8_t kf = *(__attribute__((address_space(3))) const bf16x8_t*)(
+                const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)(
                     kb + t * 32 * Y::kRow + k_base + ((32 * i) ^ k_x));
-                z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    kf, __builtin_bit_cast(bf16x8_t, q[i]), z[t], 0, 0, 0);
+                if constexpr (kBf16) {
+                    z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, q[i]), z[t],
+                        0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        z[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                            __uint_as_float(kf[x]), __uint_as_float(q[i][x]), z[t], 0, 0, 0);
+                }
             }
         }
         load(from + v_off, next_v);
@@ -347,32 +363,57 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             for (int i = 0; i < kOut; ++i) o[i] *= f;
         }
         const float ref = m == -INFINITY ? 0.0f : m;      // nothing seen yet: all p are 0
-        u32x4 p[kBN / 16];                // 16 tokens each, as the second product takes them
+        if constexpr (kBf16) {
+            u32x4 p[kBN / 16];            // 16 tokens each, as the second product takes them
 #pragma unroll
-        for (int t = 0; t < kBN / 32; ++t)
+            for (int t = 0; t < kBN / 32; ++t)
 #pragma unroll
-            for (int x = 0; x < 16; x += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x], c, -ref));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x + 1], c, -ref));
-                l += e0;
-                l += e1;
-                p[2 * t + x / 8][(x % 8) / 2] = pack_bf16x2_rne(e0, e1);
-            }
-        store_k((u + 1) & 1);
+                for (int x = 0; x < 16; x += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x], c, -ref));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x + 1], c, -ref));
+                    l += e0;
+                    l += e1;
+                    p[2 * t + x / 8][(x % 8) / 2] = pack_bf16x2_rne(e0, e1);
+                }
+            store_k((u + 1) & 1);
 #pragma unroll
-        for (int s4 = 0; s4 < kBN / 16; ++s4)
+            for (int s4 = 0; s4 < kBN / 16; ++s4)
 #pragma unroll
-            for (int i = 0; i < kOut; ++i) {
-                const lds_t at = vb + v_base + s4 * 16 * Y::kRow + ((64 * i) ^ v_x);
-                typedef __attribute__((address_space(3))) s16x4* tr_t;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 8 * Y::kRow));
-                const u32x2 x0 = __builtin_bit_cast(u32x2, lo), x1 = __builtin_bit_cast(u32x2, hi);
-                const u32x4 va = {x0[0], x0[1], x1[0], x1[1]};
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, p[s4]), o[i], 0,
-                    0, 0);
-            }
+                for (int i = 0; i < kOut; ++i) {
+                    const lds_t at = vb + v_base + s4 * 16 * Y::kRow + ((64 * i) ^ v_x);
+                    typedef __attribute__((address_space(3))) s16x4* tr_t;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at);
+                    const s16x4 hi =
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 8 * Y::kRow));
+                    const u32x2 x0 = __builtin_bit_cast(u32x2, lo);
+                    const u32x2 x1 = __builtin_bit_cast(u32x2, hi);
+                    const u32x4 va = {x0[0], x0[1], x1[0], x1[1]};
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8_t, va), __builtin_bit_cast(bf16x8_t, p[s4]),
+                        o[i], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < kBN / 32; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    z[t][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][x], c, -ref));
+                    l += z[t][x];
+                }
+            store_k((u + 1) & 1);
+            // element x of the two halves: tokens 8 (x / 4) + x % 4 and the fourth on
+#pragma unroll
+            for (int t = 0; t < kBN / 32; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+#pragma unroll
+                    for (int i = 0; i < kOut; ++i)
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                            *(__attribute__((address_space(3))) const float*)(
+                                vb + v_base + (32 * t + 8 * (x / 4) + x % 4) * Y::kRow +
+                                ((128 * i) ^ v_x)),
+                            z[t][x], o[i], 0, 0, 0);
+        }
         if (s_fix[u & 1] == u) {
             // the values that were kept out reach the rows that see them (their
             // probabilities are positive), from the cache
@@ -381,17 +422,21 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
             for (int j = 0; j < kBN; ++j) {
                 const int page = __builtin_amdgcn_readlane(here.page, j >> 4);
                 const char* raw = a.kv + (int64_t)page * a.page_stride + head_off + v_off +
-                                  (int64_t)((j0 + j) & ((1 << a.ps_log2) - 1)) * Y::kRow + half * 8;
+                                  (int64_t)((j0 + j) & ((1 << a.ps_log2) - 1)) * Y::kRow +
+                                  half * 4 * Y::kBytes;
                 if (!sees(j0 + j)) continue;
 #pragma unroll
                 for (int i = 0; i < kOut; ++i)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const u32x2 w = *(const u32x2*)(raw + i * 64 + x * 16);
+                        const char* four = raw + (32 * i + 8 * x) * Y::kBytes;
 #pragma unroll
                         for (int y = 0; y < 4; ++y) {
-                            const float v = __uint_as_float(y & 1 ? w[y / 2] & 0xFFFF0000u
-                                                                  : w[y / 2] << 16);
+                            float v;
+                            if constexpr (kBf16)
+                                v = __uint_as_float((uint32_t)((const uint16_t*)four)[y] << 16);
+                            else
+                                v = ((const float*)four)[y];
                             if (!(fabsf(v) < INFINITY)) o[i][4 * x + y] += v;
                         }
                     }
@@ -450,15 +495,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     if (!live) return;
     const int64_t at = q_row * a.n_heads + q_head;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;      // a row that sees nothing is 0
-    char* to = a.out + at * Y::kRow + half * 8;
+    char* to = a.out + at * Y::kRow + half * 4 * Y::kBytes;
 #pragma unroll
     for (int i = 0; i < kOut; ++i)
 #pragma unroll
         for (int x = 0; x < 16; x += 4) {
-            u32x2 w;
-            w[0] = pack_bf16x2_rne(o[i][x] * inv, o[i][x + 1] * inv);
-            w[1] = pack_bf16x2_rne(o[i][x + 2] * inv, o[i][x + 3] * inv);
-            *(u32x2*)(to + i * 64 + x * 4) = w;
+            const float y[4] = {o[i][x] * inv, o[i][x + 1] * inv, o[i][x + 2] * inv,
+                                o[i][x + 3] * inv};
+            store_out<kDtype, 4>(to + (32 * i + 2 * x) * Y::kBytes, y);
         }
     if (a.lse && half == 0)
         a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -527,18 +571,26 @@ __global__ __launch_bounds__(kThreads) void store_tokens_kernel(AttendArgs a, in
 // an upper bound: every request has one block at most that is not full
 int64_t tile_blocks(int64_t n_rows, int g, int n_seq) { return n_rows * g / kBM + n_seq; }
 
-template <int D>
+template <int kDtype, int D>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
     const int64_t grid = tile_blocks(a.n_rows, a.g, a.n_seq) * a.n_kv * a.splits;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     const int store = a.n_rows > 4096 ? 4 : 1;
     hipLaunchKernelGGL(store_tokens_kernel, dim3((a.n_rows + store - 1) / store), dim3(kThreads),
-                       0, stream, a, 2 * D, store);
+                       0, stream, a, Lay<kDtype, D>::kRow, store);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_tiles_kernel<D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
+    hipLaunchKernelGGL((attend_tiles_kernel<kDtype, D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
                        a);
     return hipGetLastError();
+}
+
+template <int kDtype>
+hipError_t launch_tiles_of(const AttendArgs& a, int head_dim, hipStream_t stream) {
+    if (head_dim == 64) return launch_tiles<kDtype, 64>(a, stream);
+    if constexpr (kDtype == STAR_BF16)
+        if (head_dim == 256) return launch_tiles<kDtype, 256>(a, stream);
+    return launch_tiles<kDtype, 128>(a, stream);
 }
 
 }  // namespace
@@ -548,7 +600,8 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
     const int64_t rows = (int64_t)p.n_rows * g;
     // workgroups, if the requests' last blocks are half full
     const int64_t groups = (rows + (int64_t)p.n_seq * kBM / 2) / kBM * p.n_kv_heads;
-    pl.tiled = p.dtype == STAR_BF16 && groups >= 112;
+    // (256 wide in fp32, queries and output alone fill the registers)
+    pl.tiled = groups >= 112 && !(p.dtype == STAR_F32 && p.head_dim == 256);
     // Two fit a CU; launches that leave places free cut the keys
     pl.splits = 1;
     const int64_t most = tile_blocks(p.n_rows, g, p.n_seq) * p.n_kv_heads;
@@ -556,7 +609,7 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
         // (no more than the longest request the page table holds could use:
         // workgroups that find nothing to do crowd the others' CUs, 38 -> 45 us
         // for 512 rows after 512 tokens)
-        const int tile = p.head_dim == 256 ? Lay<256>::kBN : Lay<128>::kBN;
+        const int e = p.dtype == STAR_BF16 ? 2 : 4, tile = p.head_dim * e > 256 ? 32 : 64;
         const int64_t longest = (int64_t)p.max_pages * p.page_size / tile / kPartTiles;
         pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / groups, longest));
     }
@@ -566,10 +619,9 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
                                              kThreads * sizeof(float);
 }
 
-hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream) {
-    if (head_dim == 64) return launch_tiles<64>(a, stream);
-    if (head_dim == 128) return launch_tiles<128>(a, stream);
-    return launch_tiles<256>(a, stream);
+hipError_t launch_attend_tiles(const AttendArgs& a, int dtype, int head_dim, hipStream_t stream) {
+    return dtype == STAR_BF16 ? launch_tiles_of<STAR_BF16>(a, head_dim, stream)
+                              : launch_tiles_of<STAR_F32>(a, head_dim, stream);
 }
 
 }  // namespace star

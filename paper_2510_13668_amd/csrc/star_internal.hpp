@@ -201,7 +201,7 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode);
 hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype, int head_dim,
                          hipStream_t stream);
 
-hipError_t launch_attend_tiles(const AttendArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_attend_tiles(const AttendArgs& a, int dtype, int head_dim, hipStream_t stream);
 
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t stream);
 

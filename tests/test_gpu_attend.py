@@ -217,7 +217,7 @@ def test_prompt(lens, new, Hq, Hkv, D, dtype):
 
 
 # Enough key-value heads put small prompts on the tiled kernel, which takes
-# bf16 calls of 112 workgroups (128 rows of one head each) and more.
+# calls of 112 workgroups (128 rows of one head each) and more.
 WIDE = 112
 
 
@@ -229,10 +229,11 @@ def tiled(c):
 
 @pytest.mark.parametrize("lens,new", [([1], [64]), ([17, 64, 5], [17, 30, 1]), ([100], [100]),
                                       ([200, 0, 16, 80], [130, 0, 16, 33]), ([260], [129])])
-@pytest.mark.parametrize("g,D", [(1, 64), (2, 128), (1, 256)])
-def test_prompt_tiled(lens, new, g, D):
+@pytest.mark.parametrize("g,D,dtype", [(1, 64, "bf16"), (2, 128, "bf16"), (1, 256, "bf16"),
+                                       (2, 64, "f32"), (1, 128, "f32")])
+def test_prompt_tiled(lens, new, g, D, dtype):
     lens = [max(a, b) for a, b in zip(lens, new)]
-    c = Cache(sum(lens), lens, new, WIDE * g, WIDE, D, ps=16 if D < 256 else 32, peak=2.0)
+    c = Cache(sum(lens), lens, new, WIDE * g, WIDE, D, dtype, ps=16 if D < 256 else 32, peak=2.0)
     assert tiled(c)
     check(c, False)
     check(c, False, window=29, sinks=3)
@@ -240,8 +241,9 @@ def test_prompt_tiled(lens, new, g, D):
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (64, 0), (70, 70), (64, 1),
                                           (2 ** 31 - 1, 3), (50, 2 ** 31 - 1), (100, 33)])
-def test_prompt_tiled_windows(window, sinks):
-    c = Cache(7, [190, 160], [100, 31], WIDE, WIDE, 64)
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (64, "f32"), (128, "f32")])
+def test_prompt_tiled_windows(window, sinks, D, dtype):
+    c = Cache(7, [190, 160], [100, 31], WIDE, WIDE, D, dtype)
     c.scale = -0.2                                     # and the least products first
     assert tiled(c)
     check(c, False, window, sinks)
@@ -321,8 +323,9 @@ def test_two_streams_with_workspaces_of_their_own():
     assert torch.equal(oa.cpu(), want[0]) and torch.equal(ob.cpu(), want[1])
 
 
-def test_prompt_tiled_infinities_and_bad_contents():
-    c = Cache(4, [150, 40, 90], [70, 5, 33], WIDE, WIDE, 64)
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (64, "f32"), (128, "f32")])
+def test_prompt_tiled_infinities_and_bad_contents(D, dtype):
+    c = Cache(4, [150, 40, 90], [70, 5, 33], WIDE, WIDE, D, dtype)
     c.scale = 0.05
     assert tiled(c)
     q, k, v = c.split(c.qkv)
@@ -341,19 +344,21 @@ def test_prompt_tiled_infinities_and_bad_contents():
     check(c, False, window=25, sinks=2, flags=star.DEV_BAD_LEN | star.DEV_BAD_PAGE)
 
 
-def test_prompt_tiled_many_requests():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompt_tiled_many_requests(dtype):
     new = [1 + 37 * b % 40 for b in range(70)]
-    c = Cache(5, [n + b % 3 * 20 for b, n in enumerate(new)], new, 32, 16, 64)
+    c = Cache(5, [n + b % 3 * 20 for b, n in enumerate(new)], new, 32, 16, 64, dtype)
     assert tiled(c)
     check(c, False)
 
 
-@pytest.mark.parametrize("Hq,Hkv,D,T,past,window,sinks", [
-    (16, 16, 64, 900, 2000, 0, 0), (32, 16, 128, 450, 1700, 0, 0), (32, 16, 128, 450, 1900, 1700, 9),
-    (28, 28, 256, 490, 700, 0, 0)])
-def test_prompt_tiled_cut_keys(Hq, Hkv, D, T, past, window, sinks):
+@pytest.mark.parametrize("Hq,Hkv,D,T,past,window,sinks,dtype", [
+    (16, 16, 64, 900, 2000, 0, 0, "bf16"), (32, 16, 128, 450, 1700, 0, 0, "bf16"),
+    (32, 16, 128, 450, 1900, 1700, 9, "bf16"), (28, 28, 256, 490, 700, 0, 0, "bf16"),
+    (16, 16, 64, 900, 2000, 1990, 3, "f32"), (32, 16, 128, 450, 1700, 0, 0, "f32")])
+def test_prompt_tiled_cut_keys(Hq, Hkv, D, T, past, window, sinks, dtype):
     """Few blocks over long caches: several workgroups share a block's keys."""
-    c = Cache(6, [past + T], [T], Hq, Hkv, D, ps=64, peak=3.0)
+    c = Cache(6, [past + T], [T], Hq, Hkv, D, dtype, ps=64, peak=3.0)
     assert tiled(c) and star.attend_prompt_workspace_size(c.params(0, 0)) > 1 << 20
     a = check(c, False, window, sinks)
     b = run(c, False, window, sinks)
