@@ -598,20 +598,29 @@ hipError_t launch_tiles_of(const AttendArgs& a, int head_dim, hipStream_t stream
 void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
     const int g = p.n_heads / p.n_kv_heads;
     const int64_t rows = (int64_t)p.n_rows * g;
-    // workgroups, if the requests' last blocks are half full
+    const int e = p.dtype == STAR_BF16 ? 2 : 4;
+    // workgroups, if the requests' last blocks are half full, and the most keys
+    // that a row can see
     const int64_t groups = (rows + (int64_t)p.n_seq * kBM / 2) / kBM * p.n_kv_heads;
-    // (256 wide in fp32, queries and output alone fill the registers)
-    pl.tiled = groups >= 112 && !(p.dtype == STAR_F32 && p.head_dim == 256);
+    int64_t keys = (int64_t)p.max_pages * p.page_size;
+    if (p.window) keys = std::min(keys, (int64_t)p.window + p.sinks);
+    // Fewer workgroups leave the row-block kernel ahead, whose pieces are finer.
+    // bf16: 10 prompts of 23 tokens (104) 14.5 us against 13.8, of 70 (64) 14.6 against
+    // 17.1, 15 of 27 (56) 9.4 against 13.7; fp32: 26 against 29 at 131, 39 against 35 at
+    // 176; a few rows after thousands of tokens, whose keys are cut below, 105
+    // against 50 at 64.  (256 wide in fp32, queries and output alone fill the
+    // registers.)
+    pl.tiled = (groups >= (p.dtype == STAR_BF16 ? 112 : 160) || (groups >= 56 && keys >= 4096)) &&
+               !(p.dtype == STAR_F32 && p.head_dim == 256);
     // Two fit a CU; launches that leave places free cut the keys
     pl.splits = 1;
     const int64_t most = tile_blocks(p.n_rows, g, p.n_seq) * p.n_kv_heads;
     if (pl.tiled && groups <= 256 && most <= kMaxTickets) {
-        // (no more than the longest request the page table holds could use:
-        // workgroups that find nothing to do crowd the others' CUs, 38 -> 45 us
-        // for 512 rows after 512 tokens)
-        const int e = p.dtype == STAR_BF16 ? 2 : 4, tile = p.head_dim * e > 256 ? 32 : 64;
-        const int64_t longest = (int64_t)p.max_pages * p.page_size / tile / kPartTiles;
-        pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / groups, longest));
+        // (no more than the most keys could use: workgroups that find nothing to do
+        // crowd the others' CUs, 38 -> 45 us for 512 rows after 512 tokens)
+        const int tile = p.head_dim * e > 256 ? 32 : 64;
+        pl.splits = (int)std::max<int64_t>(
+            1, std::min<int64_t>(512 / groups, keys / tile / kPartTiles));
     }
     if (pl.tiled)
         pl.part_bytes = pl.splits == 1 ? 0
