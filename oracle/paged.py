@@ -1,8 +1,8 @@
 """Plain restatement of the paged cache's operators -- TEST INFRASTRUCTURE.
 
 Page tables: one slot and one page after the other, in order.  Attention: one
-request and row after the other over the request's tokens in a plain row, in
-64 bits.  Host tensors in and out; nothing here imports the HIP
+request after the other over its tokens in a plain row, in 64 bits, row by row
+where some are not finite.  Host tensors in and out; nothing here imports the HIP
 path.
 """
 from __future__ import annotations
@@ -168,23 +168,32 @@ def attend(q, k_new, v_new, kv, table, seq_len, q_start=None, *, scale, window=0
                 there[at] = True
             elif seen[at].any():
                 flags |= BAD_PAGE
-        for i in range(T):
-            p = L - T + i
+        def visible(p):
             see = (j <= p) & there
-            if window:
-                see &= (j > p - window) | (j < sinks)
-            jj = torch.nonzero(see).squeeze(1)
-            if jj.numel() == 0:
+            return see & ((j > p - window) | (j < sinks)) if window else see
+
+        # query head h reads key-value head h // g
+        kg, vg = (t.repeat_interleave(g, dim=0) for t in (k, v))
+        finite = bool(torch.isfinite(k).all() and torch.isfinite(v).all())
+        for at in range(0, T, 64 if finite else 1):
+            rows = slice(lo + at, lo + min(T, at + (64 if finite else 1)))
+            pos = torch.arange(L - T + at, L - T + at + rows.stop - rows.start)
+            see = torch.stack([visible(int(p)) for p in pos])          # [rows, L]
+            if finite:
+                kh, vh = kg, vg
+            else:                                    # one row, over the keys it sees
+                kh, vh, see = kg[:, see[0]], vg[:, see[0]], see[:, see[0]]
+            qh = q[rows].double().transpose(0, 1)                      # [Hq, rows, D]
+            z = (scale * (qh @ kh.transpose(1, 2))).masked_fill(~see, -math.inf)
+            if see.shape[1] == 0:
                 continue
-            # query head h reads key-value head h // g
-            kh, vh = (t[:, jj].repeat_interleave(g, dim=0) for t in (k, v))
-            qh = q[lo + i].double()[:, :, None]
-            z = scale * (kh @ qh)[:, :, 0]
-            top = z.max(dim=1).values
-            e = torch.exp(z - top[:, None])
-            pr = (e / e.sum(1, keepdim=True))[:, None]
-            out[lo + i] = (pr @ vh)[:, 0]
-            mass[lo + i] = (pr @ vh.abs())[:, 0]
-            lse[lo + i] = top + torch.log(e.sum(1))
-            reach[lo + i] = (abs(scale) * (kh.abs() @ qh.abs())[:, :, 0]).max(dim=1).values
+            top = z.max(dim=2).values
+            e = torch.exp(z - top.clamp(min=-1e300)[..., None])
+            total = e.sum(2)
+            pr = e / total.clamp(min=1e-300)[..., None]
+            out[rows] = (pr @ vh).transpose(0, 1)
+            mass[rows] = (pr @ vh.abs()).transpose(0, 1)
+            lse[rows] = (top + torch.log(total)).transpose(0, 1)
+            span = (abs(scale) * (qh.abs() @ kh.abs().transpose(1, 2))).masked_fill(~see, 0.0)
+            reach[rows] = span.max(dim=2).values.transpose(0, 1)
     return dict(out=out, lse=lse, written=written, mass=mass, reach=reach, kv=kv_out, flags=flags)

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kPartTiles = 16;   // tiles that are worth a part of their own
+constexpr int kPlaces = 512;     // workgroups that run at once, two a CU
 constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may lag
 
 typedef __attribute__((address_space(3))) char* lds_t;
@@ -175,10 +175,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
 
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
     const Tiles tl = tiles_of<kBN>(a, p0, p1);
-    // this workgroup's share of the tiles: all, or one of `parts`, which pay from
-    // about sixteen tiles each (512 rows after 16000 tokens: 416 -> 174 us; after
-    // 512, two parts of eight: 38 -> 43)
-    const int parts = max(1, min(a.splits, tl.n / kPartTiles));
+    // this workgroup's share of the tiles: all, or one of `parts`
+    const int parts = max(1, min(a.splits, tl.n / a.part_tiles));
     if (part >= parts) return;
     const int u0 = (int)((int64_t)tl.n * part / parts);
     const int u1 = (int)((int64_t)tl.n * (part + 1) / parts);
@@ -612,15 +610,36 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
     // registers.)
     pl.tiled = (groups >= (p.dtype == STAR_BF16 ? 112 : 160) || (groups >= 56 && keys >= 4096)) &&
                !(p.dtype == STAR_F32 && p.head_dim == 256);
-    // Two fit a CU; launches that leave places free cut the keys
     pl.splits = 1;
     const int64_t most = tile_blocks(p.n_rows, g, p.n_seq) * p.n_kv_heads;
-    if (pl.tiled && groups <= 256 && most <= kMaxTickets) {
+    if (pl.tiled && most <= kMaxTickets) {
+        int splits = 1;
+        if (2 * groups <= kPlaces) {
+            // Places stay free: each block's keys are cut, into parts that pay from
+            // sixteen tiles each (512 rows after 16000 tokens: 416 -> 172 us; after
+            // 512, two parts of eight tiles: 38 -> 43)
+            pl.part_tiles = 16;
+            splits = (int)(kPlaces / groups);
+        } else {
+            // Cut keys fill the last round of places better, for 4% of a round a
+            // cut; a round that leaves every CU one workgroup takes 0.62 of one.
+            // Worth it for long parts (300 workgroups over 9200 tokens: 300 -> 225
+            // us; 520: 464 -> 384; 700: 512 against 532; 640 over a window of 4096:
+            // 205 against 229)
+            pl.part_tiles = 40;
+            auto cost = [&](int s) {
+                const double rounds = (double)groups * s / kPlaces, part = rounds - (int)rounds;
+                return ((int)rounds + (part > 0.5 ? 1.0 : part > 0.0 ? 0.62 : 0.0)) / s +
+                       0.04 * (s - 1);
+            };
+            for (int s = 2; s <= 3; ++s)
+                if (cost(s) < 0.93 * cost(1) && cost(s) < cost(splits)) splits = s;
+        }
         // (no more than the most keys could use: workgroups that find nothing to do
         // crowd the others' CUs, 38 -> 45 us for 512 rows after 512 tokens)
         const int tile = p.head_dim * e > 256 ? 32 : 64;
         pl.splits = (int)std::max<int64_t>(
-            1, std::min<int64_t>(512 / groups, keys / tile / kPartTiles));
+            1, std::min<int64_t>(splits, keys / tile / pl.part_tiles));
     }
     if (pl.tiled)
         pl.part_bytes = pl.splits == 1 ? 0

@@ -186,14 +186,16 @@ struct AttendArgs {
     int ps_log2, n_pages, max_pages, window, sinks;
     float scale_log2;           // scale * log2(e)
     int min_steps;
-    int splits;                 // the tiled kernel: parts of a block's keys at most
+    int splits, part_tiles;     // the tiled kernel: parts of a block's keys at most, and
+                                // the fewest tiles of one
 };
 struct AttendPlan {
     int grid = 0;               // workgroups of the row-block kernel
     int min_steps = 1;          // steps that a workgroup takes at least
     size_t part_bytes = 0;
     bool tiled = false;         // the kernel of attend_prompt.hip
-    int splits = 1;             // the most parts it cuts a block's keys into
+    int splits = 1;             // the most parts it cuts a block's keys into,
+    int part_tiles = 16;        // of this many tiles at least
 };
 // whether and how attend_prompt.hip's kernel takes a call
 void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl);

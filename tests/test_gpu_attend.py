@@ -356,7 +356,7 @@ def test_prompt_tiled_many_requests(dtype):
     (16, 16, 64, 900, 2000, 0, 0, "bf16"), (32, 16, 128, 450, 1700, 0, 0, "bf16"),
     (32, 16, 128, 450, 1900, 1700, 9, "bf16"), (28, 28, 256, 490, 700, 0, 0, "bf16"),
     (24, 24, 64, 900, 2000, 1990, 3, "f32"), (48, 24, 128, 450, 1700, 0, 0, "f32"),
-    (8, 8, 64, 900, 4000, 0, 0, "bf16")])
+    (8, 8, 64, 900, 4000, 0, 0, "bf16"), (96, 96, 64, 340, 5100, 0, 0, "bf16")])
 def test_prompt_tiled_cut_keys(Hq, Hkv, D, T, past, window, sinks, dtype):
     """Few blocks over long caches: several workgroups share a block's keys."""
     c = Cache(6, [past + T], [T], Hq, Hkv, D, dtype, ps=64, peak=3.0)
