@@ -423,7 +423,7 @@ star_status star_plan_migrations(const star_plan_params* p, const int32_t* cur_l
  * written.
  * ---------------------------------------------------------------------- */
 typedef struct {
-    int32_t n_seq;        /* slots >= 0 */
+    int32_t n_seq;        /* slots, 0 .. 2^30 */
     int32_t max_pages;    /* columns of the page table >= 1;
                              max_pages * page_size <= 2^30 */
     int32_t n_pages;      /* pages of the pool >= 1, a multiple of n_inst, <= 2^30 */
@@ -513,9 +513,10 @@ star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
  * index out of range are left out (STAR_DEV_BAD_PAGE).
  * ---------------------------------------------------------------------- */
 typedef struct {
-    int32_t n_seq;       /* slots >= 0 */
+    int32_t n_seq;       /* slots, 0 .. 2^30 */
     int32_t n_rows;      /* rows of q: n_seq (decode); all new tokens (prompt) */
-    int32_t n_heads;     /* query heads, a multiple of n_kv_heads */
+    int32_t n_heads;     /* query heads, a multiple of n_kv_heads, <= 65536;
+                            n_rows * n_heads < 2^31 */
     int32_t n_kv_heads;  /* >= 1 */
     int32_t head_dim;    /* 64, 128 or 256 */
     int32_t dtype;       /* star_dtype of q, k_new, v_new, kv and out */
@@ -524,7 +525,7 @@ typedef struct {
     int32_t max_pages;   /* columns of the page table; max_pages * page_size <= 2^30 */
     int32_t window;      /* >= 0; 0: none */
     int32_t sinks;       /* >= 0 first tokens that stay visible under a window */
-    float   scale;       /* finite */
+    float   scale;       /* finite, and in powers of two (scale log2 e) too */
     int64_t q_stride;    /* elements between rows of q (a multiple of 16 bytes) */
     int64_t kv_stride;   /* elements between rows of k_new and of v_new (the same) */
     int64_t page_stride; /* bytes between pages, a multiple of 16 */

@@ -487,7 +487,8 @@ static star_status check_pages_params(const star_pages_params* p) {
         p->page_bytes < 1 || p->page_size < 1)
         return STAR_ERR_INVALID_ARG;
     if (p->n_pages % p->n_inst) return STAR_ERR_INVALID_ARG;
-    if (!page_size_ok(p->page_size) || p->n_inst > 1024 || p->n_pages > 1 << 30)
+    if (!page_size_ok(p->page_size) || p->n_inst > 1024 || p->n_pages > 1 << 30 ||
+        p->n_seq > 1 << 30)
         return STAR_ERR_UNSUPPORTED;
     if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return STAR_ERR_UNSUPPORTED;
     if (p->page_bytes % 16 || p->page_stride % 16 || p->layer_stride % 16)
@@ -556,20 +557,26 @@ STAR_API star_status star_compact_pages(const star_pages_params* p, const int32_
 // ---------------------------------------------------------------------------
 // attention over the cache
 // ---------------------------------------------------------------------------
+// the scale of scores in powers of two
+static float scale_log2(const star_attend_params& p) {
+    return (float)((double)p.scale * 1.4426950408889634);
+}
+
 static star_status check_attend_params(const star_attend_params* p) {
     if (!p) return STAR_ERR_INVALID_ARG;
     if (p->n_seq < 0 || p->n_rows < 0 || p->n_heads < 1 || p->n_kv_heads < 1 || p->head_dim < 1 ||
         p->page_size < 1 || p->n_pages < 1 || p->max_pages < 1 || p->window < 0 || p->sinks < 0)
         return STAR_ERR_INVALID_ARG;
     if (p->dtype != STAR_F32 && p->dtype != STAR_BF16) return STAR_ERR_INVALID_ARG;
-    if (p->n_heads % p->n_kv_heads || !isfinite(p->scale)) return STAR_ERR_INVALID_ARG;
+    if (p->n_heads % p->n_kv_heads || !isfinite(scale_log2(*p))) return STAR_ERR_INVALID_ARG;
     const int64_t e = p->dtype == STAR_BF16 ? 2 : 4;
     const __int128 page = (__int128)2 * p->n_kv_heads * p->page_size * p->head_dim * e;
     if (p->q_stride < (int64_t)p->n_heads * p->head_dim ||
         p->kv_stride < (int64_t)p->n_kv_heads * p->head_dim || p->page_stride < page)
         return STAR_ERR_INVALID_ARG;
     if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return STAR_ERR_UNSUPPORTED;
-    if (!page_size_ok(p->page_size)) return STAR_ERR_UNSUPPORTED;
+    if (!page_size_ok(p->page_size) || p->n_seq > 1 << 30 || p->n_heads > 1 << 16)
+        return STAR_ERR_UNSUPPORTED;
     if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return STAR_ERR_UNSUPPORTED;
     if (p->q_stride * e % 16 || p->kv_stride * e % 16 || p->page_stride % 16)
         return STAR_ERR_UNSUPPORTED;
@@ -612,7 +619,7 @@ static star_status attend(const star_attend_params* p, const void* q, const void
     a.g = p->n_heads / p->n_kv_heads;
     a.ps_log2 = __builtin_ctz(p->page_size), a.n_pages = p->n_pages, a.max_pages = p->max_pages;
     a.window = p->window, a.sinks = p->sinks;
-    a.scale_log2 = (float)((double)p->scale * 1.4426950408889634);
+    a.scale_log2 = scale_log2(*p);
     const hipError_t err = launch_attend(pl, a, p->dtype, p->head_dim, (hipStream_t)stream);
     return err == hipSuccess ? STAR_OK : STAR_ERR_HIP;
 }

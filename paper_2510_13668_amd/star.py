@@ -8,6 +8,7 @@ the library is missing, importing the binding's entry points raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -194,11 +195,33 @@ def _ptr(t: Optional[torch.Tensor]):
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _same_device(t: torch.Tensor, stream):
-    """The tensor's device is the current one, and the stream's."""
+def _same_device(t: torch.Tensor, stream, *others):
+    """The tensor's device (returned) is the current one, the stream's and the
+    others'."""
     dev = t.get_device()
     if dev != torch.cuda.current_device() or (stream is not None and stream.device_index != dev):
         raise ValueError("the tensors' device has to be the current one and the stream's")
+    for x in others:
+        if x.get_device() != dev:
+            raise ValueError("the tensors and the workspace have to be on one device")
+    return dev
+
+
+def _arrays(dev: int, wants, *ts):
+    """The addresses of contiguous tensors on device dev, each of its (type, least
+    bytes) in wants; None stays None."""
+    out = []
+    for t, (dtype, n) in zip(ts, wants):
+        if t is None:
+            out.append(None)
+            continue
+        if (t.get_device() != dev or t.dtype is not dtype or t.nbytes < n or
+                not t.is_contiguous()):
+            raise ValueError(f"expected a contiguous tensor of {dtype} and {n} bytes on device "
+                             f"{dev}, got {t.dtype}, {t.nbytes} bytes, strides {t.stride()} on "
+                             f"device {t.get_device()}")
+        out.append(t.data_ptr())
+    return out
 
 
 def _stream(stream) -> int:
@@ -418,6 +441,24 @@ def pages_params(n_seq, max_pages, n_pages, page_size, n_layers, page_bytes, n_i
                        page_stride, layer_stride)
 
 
+@functools.lru_cache(maxsize=256)
+def _pages_layout(fields: bytes):
+    """What the calls take with these parameters: the (type, bytes) of an array per
+    slot, of tables, counts and live pages, and the pool's bytes (by value: see
+    _attend_layout)."""
+    p = PagesParams.from_buffer_copy(fields)
+    pool = (p.n_layers - 1) * p.layer_stride + (p.n_pages - 1) * p.page_stride + p.page_bytes
+    ints = (p.n_seq, p.n_seq * p.max_pages, p.n_pages, p.n_inst)
+    return *((torch.int32, 4 * n) for n in ints), pool
+
+
+def _pool(kv, nbytes: int) -> int:
+    """The address of a contiguous pool of at least this many bytes."""
+    if kv.nbytes < nbytes or not kv.is_contiguous():
+        raise ValueError(f"the pool has to be contiguous and of {nbytes} bytes, got {kv.nbytes}")
+    return kv.data_ptr()
+
+
 def assign_pages_workspace_size(p: PagesParams) -> int:
     return int(lib().star_assign_pages_workspace_size(ctypes.byref(p)))
 
@@ -428,10 +469,16 @@ def assign_pages(p: PagesParams, parent, new_len, inst_of, table, seq_len, seq_i
     instance.  parent, inst_of: None for none; seq_inst, seq_inst_out may be
     None where p.n_inst is 1.  Outputs may be their inputs (table_out only
     without parents)."""
-    _same_device(kv, stream)
+    dev = _same_device(kv, stream, ws.buf)
+    slots, tables, counts, _, pool = _pages_layout(bytes(p))
+    (parent, new_len, inst_of, table, seq_len, seq_inst, refs, table_out, seq_len_out,
+     seq_inst_out, refs_out) = _arrays(
+         dev, (slots, slots, slots, tables, slots, slots, counts, tables, slots, slots, counts),
+         parent, new_len, inst_of, table, seq_len, seq_inst, refs, table_out, seq_len_out,
+         seq_inst_out, refs_out)
     _check("star_assign_pages", lib().star_assign_pages(
-        ctypes.byref(p), *_ptrs(parent, new_len, inst_of, table, seq_len, seq_inst, refs,
-                                kv, table_out, seq_len_out, seq_inst_out, refs_out),
+        ctypes.byref(p), parent, new_len, inst_of, table, seq_len, seq_inst, refs,
+        _pool(kv, pool), table_out, seq_len_out, seq_inst_out, refs_out,
         ws.ptr, ws.nbytes, _stream(stream)))
 
 
@@ -442,9 +489,13 @@ def compact_pages_workspace_size(p: PagesParams) -> int:
 def compact_pages(p: PagesParams, table, seq_len, refs, kv, table_out, refs_out, n_live,
                   ws: Workspace, stream=None):
     """star_compact_pages: every instance's live pages to its lowest indices."""
-    _same_device(kv, stream)
+    dev = _same_device(kv, stream, ws.buf)
+    slots, tables, counts, insts, pool = _pages_layout(bytes(p))
+    table, seq_len, refs, table_out, refs_out, n_live = _arrays(
+        dev, (tables, slots, counts, tables, counts, insts),
+        table, seq_len, refs, table_out, refs_out, n_live)
     _check("star_compact_pages", lib().star_compact_pages(
-        ctypes.byref(p), *_ptrs(table, seq_len, refs, kv, table_out, refs_out, n_live),
+        ctypes.byref(p), table, seq_len, refs, _pool(kv, pool), table_out, refs_out, n_live,
         ws.ptr, ws.nbytes, _stream(stream)))
 
 
@@ -468,11 +519,11 @@ def attend_params(n_seq, n_rows, n_heads, n_kv_heads, head_dim, dtype, page_size
 _TORCH_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
 
-def _strided(t: torch.Tensor, dtype, shape, strides) -> int:
-    """The address of a device tensor of this shape and these strides (the
-    steps of dimensions of size 1 are any)."""
-    if not t.is_cuda:
-        raise ValueError("libstar takes device tensors")
+def _strided(t: torch.Tensor, dtype, shape, strides, dev=None) -> int:
+    """The address of a tensor (on device dev, if given) of this shape and these
+    strides (the steps of dimensions of size 1 are any)."""
+    if not t.is_cuda if dev is None else t.get_device() != dev:
+        raise ValueError("libstar takes device tensors, all on one device")
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
     got = t.stride()
@@ -481,13 +532,31 @@ def _strided(t: torch.Tensor, dtype, shape, strides) -> int:
     return t.data_ptr()
 
 
-def _attend_ptrs(p: AttendParams, q, k_new, v_new, kv):
+@functools.lru_cache(maxsize=256)
+def _attend_layout(fields: bytes):
+    """What a call with these parameters takes: its type, shapes and strides of q,
+    k_new and v_new, and kv, and the (type, bytes) of its other arrays (by value,
+    since a dozen reads of a ctypes structure take 1 us of a small call's 8)."""
+    p = AttendParams.from_buffer_copy(fields)
     dt, D, n, Hkv, ps = _TORCH_DTYPES[p.dtype], p.head_dim, p.n_rows, p.n_kv_heads, p.page_size
-    new, rows = (n, Hkv, D), (p.kv_stride, D, 1)
-    return (_strided(q, dt, (n, p.n_heads, D), (p.q_stride, D, 1)),
-            _strided(k_new, dt, new, rows), _strided(v_new, dt, new, rows),
-            _strided(kv, dt, (p.n_pages, 2, Hkv, ps, D),
-                     (p.page_stride // dt.itemsize, Hkv * ps * D, ps * D, D, 1)))
+    i32 = torch.int32
+    return (dt, (n, p.n_heads, D), (p.q_stride, D, 1), (n, Hkv, D), (p.kv_stride, D, 1),
+            (p.n_pages, 2, Hkv, ps, D),
+            (p.page_stride // dt.itemsize, Hkv * ps * D, ps * D, D, 1),
+            ((i32, 4 * p.n_seq * p.max_pages), (i32, 4 * p.n_seq)), ((i32, 4 * p.n_seq + 4),),
+            ((dt, n * p.n_heads * D * dt.itemsize), (torch.float32, 4 * n * p.n_heads)))
+
+
+def _attend_ptrs(p: AttendParams, q, k_new, v_new, kv, table, seq_len, starts, out, lse, dev):
+    """The addresses of a call's tensors, in the order of its arguments (starts:
+    (q_start,), or none)."""
+    (dt, q_shape, q_strides, new_shape, new_strides, kv_shape, kv_strides, ints, start,
+     outs) = _attend_layout(bytes(p))
+    return (_strided(q, dt, q_shape, q_strides, dev),
+            _strided(k_new, dt, new_shape, new_strides, dev),
+            _strided(v_new, dt, new_shape, new_strides, dev),
+            _strided(kv, dt, kv_shape, kv_strides, dev),
+            *_arrays(dev, ints + start[:len(starts)] + outs, table, seq_len, *starts, out, lse))
 
 
 def attend_decode_workspace_size(p: AttendParams) -> int:
@@ -500,10 +569,11 @@ def attend_decode(p: AttendParams, q, k_new, v_new, kv, table, seq_len, out, lse
     heads, head_dim], rows p.q_stride and p.kv_stride elements apart (columns
     of one projection's output do); kv: one layer of the pool, [n_pages, 2,
     n_kv_heads, page_size, head_dim]; lse: None for none."""
-    _same_device(kv, stream)
+    dev = _same_device(kv, stream, ws.buf)
     _check("star_attend_decode", lib().star_attend_decode(
-        ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
-        *_ptrs(table, seq_len, out, lse), ws.ptr, ws.nbytes, _stream(stream)))
+        ctypes.byref(p),
+        *_attend_ptrs(p, q, k_new, v_new, kv, table, seq_len, (), out, lse, dev),
+        ws.ptr, ws.nbytes, _stream(stream)))
 
 
 def attend_prompt_workspace_size(p: AttendParams) -> int:
@@ -515,7 +585,8 @@ def attend_prompt(p: AttendParams, q, k_new, v_new, kv, table, seq_len, q_start,
     """star_attend_prompt: several new tokens a slot, rows q_start[b] ..
     q_start[b + 1] - 1 of q, k_new, v_new, out and lse; otherwise as
     attend_decode."""
-    _same_device(kv, stream)
+    dev = _same_device(kv, stream, ws.buf)
     _check("star_attend_prompt", lib().star_attend_prompt(
-        ctypes.byref(p), *_attend_ptrs(p, q, k_new, v_new, kv),
-        *_ptrs(table, seq_len, q_start, out, lse), ws.ptr, ws.nbytes, _stream(stream)))
+        ctypes.byref(p),
+        *_attend_ptrs(p, q, k_new, v_new, kv, table, seq_len, (q_start,), out, lse, dev),
+        ws.ptr, ws.nbytes, _stream(stream)))

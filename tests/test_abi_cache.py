@@ -52,7 +52,7 @@ def _compact(L, p, ws_bytes=BIG, ws=FAKE, **ptrs):
     (dict(page_size=8), -2), (dict(page_size=48), -2), (dict(page_size=512), -2),
     (dict(n_inst=2048, n_pages=2048), -2), (dict(page_bytes=24), -2), (dict(page_stride=72), -2),
     (dict(layer_stride=4104), -2), (dict(max_pages=(1 << 26) + 1), -2),
-    (dict(page_stride=1 << 60, layer_stride=1 << 60), -3),
+    (dict(page_stride=1 << 60, layer_stride=1 << 60), -3), (dict(n_seq=(1 << 30) + 1), -2),
 ])
 def test_page_calls_reject_bad_scalars(L, kw, status):
     p = _pages(**kw)
@@ -113,6 +113,8 @@ def _prompt(L, p, ws_bytes=BIG, ws=FAKE, **ptrs):
     (dict(page_size=512), -2), (dict(q_stride=1028), -2), (dict(kv_stride=260), -2),
     (dict(page_stride=(1 << 20) + 8), -2), (dict(max_pages=(1 << 26) + 1), -2),
     (dict(n_seq=1 << 28, n_rows=1 << 28), -3), (dict(page_stride=1 << 60), -3),
+    (dict(n_seq=(1 << 30) + 1, n_rows=(1 << 30) + 1, n_heads=1, n_kv_heads=1), -2),
+    (dict(n_heads=1 << 17), -2), (dict(scale=3e38), -1),
 ])
 def test_attention_rejects_bad_scalars(L, kw, status):
     p = _attend(**kw)
@@ -168,6 +170,41 @@ def test_binding_refuses_another_device(monkeypatch):
     for tensor, stream in ((On(0), None), (On(1), On(0)), (On(0), On(0))):
         with pytest.raises(ValueError):
             star._same_device(tensor, stream)
+
+
+    star._same_device(On(1), None, On(1))
+    with pytest.raises(ValueError):
+        star._same_device(On(1), None, On(1), On(-1))
+
+
+def test_binding_refuses_short_and_mistyped_arrays():
+    class At(_Meta):
+        def get_device(self):
+            return 3
+
+    i32 = torch.int32
+    t = torch.zeros((4, 5), dtype=i32)
+    assert star._arrays(3, ((i32, 80), (i32, 7)), At(t), None) == [t.data_ptr(), None]
+    for bad, n in ((At(t), 81), (At(t.long()), 80), (At(t.t()), 80), (t, 80)):
+        with pytest.raises(ValueError):
+            star._arrays(3, ((i32, n),), bad)
+    # a pool of two layers of ten pages
+    pool = star._pages_layout(bytes(star.pages_params(1, 1, 10, 16, 2, 64)))[-1]
+    assert pool == 1280
+    kv = torch.empty(pool, dtype=torch.uint8)
+    assert star._pool(kv, pool) == kv.data_ptr()
+    for bad in (kv[1:], torch.empty((40, 64), dtype=torch.uint8).t()):
+        with pytest.raises(ValueError):
+            star._pool(bad, pool)
+
+
+def test_binding_follows_changed_parameters():
+    p = _attend()
+    before = star._attend_layout(bytes(p))
+    p.n_rows = p.n_seq = 5
+    after = star._attend_layout(bytes(p))
+    assert before[1] == (4, 8, 128) and after[1] == (5, 8, 128)
+    assert star._attend_layout(bytes(_attend())) == before
 
 
 class _Meta:
