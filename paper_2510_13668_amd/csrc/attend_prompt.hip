@@ -151,7 +151,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int p0 = pos_of(row_from), p1 = pos_of(row_from + kBM - 1);       // the workgroup's
     const int wave_row = row_from + 32 * wave;
     const int w0 = pos_of(wave_row), w1 = pos_of(wave_row + 31);            // the wave's
-    const bool active = wave_row < all_rows;
     const bool live = wave_row + r32 < all_rows;
     const int row = min(wave_row + r32, all_rows - 1);
     const int pos = live ? first + row / a.g : -1;
