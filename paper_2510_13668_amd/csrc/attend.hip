@@ -689,6 +689,7 @@ hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype
     a.min_steps = pl.min_steps;
     a.splits = pl.splits;
     a.part_tiles = pl.part_tiles;
+    a.items = pl.items;
     if (a.n_seq == 0 || a.n_rows == 0) return hipSuccess;
     if (pl.tiled) return launch_attend_tiles(a, dtype, head_dim, stream);
     if (dtype == STAR_BF16) {

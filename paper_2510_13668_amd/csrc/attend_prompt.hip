@@ -13,6 +13,9 @@ namespace {
 constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kPlaces = 512;     // workgroups that run at once, two a CU
+constexpr int kMaxParts = 8;     // parts of a block's keys at most
+constexpr int kMoreParts = 512;  // of a launch's longer blocks, beside those the host counts
+constexpr int kPartTiles = 16;   // and the fewest tiles of one: shorter ones do not pay
 constexpr float kLazy = 8.0f;    // log2 of the factor that a stale maximum may lag
 
 typedef __attribute__((address_space(3))) char* lds_t;
@@ -80,14 +83,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int r32 = lane & 31, half = lane >> 5;
 
-    // which request and which of its blocks of rows: those with the longest
-    // prefixes first, so that the launch ends on short ones
-    const int head = blockIdx.x % a.n_kv;
-    const int part = blockIdx.x / a.n_kv % a.splits, nth = blockIdx.x / a.n_kv / a.splits;
-    int b, block;
+    // which request, which of its blocks of rows and which part of the block's keys:
+    // those with the longest prefixes first, so that the launch ends on short ones
+    const int head = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
+    int b, block, nth, part = 0, parts = 1;
     if (a.n_seq <= 64) {
-        // one request a lane, every wave by itself: the largest last position X
-        // that more than nth blocks reach, then the blocks at X in order
+        // one request a lane, every wave by itself
         int32_t bad = 0;
         Slot s = {0, 0, 0, 0, 0};
         if (lane < a.n_seq) s = slot_of<kBN>(a, lane, bad);
@@ -102,7 +103,53 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         auto all = [&](int mine) {
             return __builtin_amdgcn_readlane(wave_incl_add_i32(mine), 63);
         };
-        if (nth >= all(n)) return;
+        // Where the host cuts at all: blocks with a last position of X or more have
+        // k parts or more, for an X that grows with k; count[k] of them, the first in
+        // the order, so that no workgroup is without work (4 requests of 600 after 0 to
+        // 6000 tokens: 247 us where a block's spare parts ended early, now 200).  A
+        // block is cut as the host says, or into more where it is longer than a place's
+        // fair share of all tiles (3 requests of 300 after 0 to 16000: 217 -> 182); the
+        // share grows until the parts fit the launch.
+        int count[kMaxParts + 2] = {};
+        count[1] = all(n);
+        int64_t sum = count[1];
+        const int cap = a.window && a.sinks < (1 << 30) - a.window ? a.window + a.sinks : 1 << 30;
+        auto tiles = [&](int x) { return min(x, cap) / kBN; };
+        if (a.splits > 1 && __any(tiles(s.L) >= 2 * kPartTiles)) {
+            int64_t total = (int64_t)n * ((tiles(s.L - s.T) + tiles(s.L)) / 2 + 1);
+            total = readlane_i64(wave_incl_add_i64(total), 63) * a.n_kv /
+                    (D == 256 ? kPlaces / 2 : kPlaces);
+            constexpr int kMost = 1 << 26;
+            int share = (int)min((int64_t)kMost, max((int64_t)kPartTiles, total));
+            for (;; share *= 2) {
+                sum = count[1];
+#pragma unroll
+                for (int k = 2; k <= kMaxParts; ++k) {
+                    int least = max(kPartTiles * k, (k - 1) * share + 1);
+                    if (k <= a.splits) least = min(least, a.part_tiles * k);
+                    count[k] = least > cap / kBN ? 0 : all(reach(least * kBN - 1));
+                    sum += count[k];
+                }
+                if (sum <= a.items && (int64_t)count[2] * a.n_kv <= kMaxTickets) break;
+                if (share >= kMost) {          // (only where ranges of rows overlap)
+#pragma unroll
+                    for (int k = 2; k <= kMaxParts; ++k) count[k] = 0;
+                    sum = count[1];
+                    break;
+                }
+            }
+        }
+        if (item >= sum) return;
+        nth = item;
+        int at = item;
+#pragma unroll
+        for (int k = kMaxParts; k > 0; --k) {
+            const int here = (count[k] - count[k + 1]) * k;      // parts of blocks of k
+            if (at >= 0 && at < here) nth = count[k + 1] + at / k, part = at % k, parts = k;
+            at -= here;
+        }
+        // the largest last position X that more than nth blocks reach, then the
+        // blocks at X in order
         int lo = 0, hi = 64;
         while (__any(hi < s.L)) hi <<= 1;                // (L is at most 2^30)
         while (hi - lo > 1) {
@@ -116,6 +163,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         b = __builtin_ctzll(past);
         block = __builtin_amdgcn_readlane(n - reach(lo) + rank - (upto - here), b);
     } else {
+        nth = item / a.splits, part = item - nth * a.splits;
         const int per = (a.n_seq + kThreads - 1) / kThreads;
         int64_t mine = 0, total;
         int32_t bad = 0;
@@ -175,7 +223,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
     const Tiles tl = tiles_of<kBN>(a, p0, p1);
     // this workgroup's share of the tiles: all, or one of `parts`
-    const int parts = max(1, min(a.splits, tl.n / a.part_tiles));
+    if (a.n_seq > 64) parts = max(1, min(a.splits, tl.n / a.part_tiles));
     if (part >= parts) return;
     const int u0 = (int)((int64_t)tl.n * part / parts);
     const int u1 = (int)((int64_t)tl.n * (part + 1) / parts);
@@ -453,7 +501,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         constexpr uint32_t kBytes = kPartFloats<D> * kThreads * 4;
         const uint32_t id = (uint32_t)(nth * a.n_kv + head);
         const __amdgpu_buffer_rsrc_t ws =
-            xch_rsrc(a.part + (size_t)id * a.splits * kBytes, (uint32_t)parts * kBytes);
+            xch_rsrc(a.part + ((size_t)head * a.items + (item - part)) * kBytes,
+                     (uint32_t)parts * kBytes);
         const uint32_t mine = (uint32_t)part * kBytes + tid * 16;
         xch_store(u32x4{__float_as_uint(m), __float_as_uint(l), 0, 0}, ws, mine);
 #pragma unroll
@@ -570,15 +619,15 @@ int64_t tile_blocks(int64_t n_rows, int g, int n_seq) { return n_rows * g / kBM 
 
 template <int kDtype, int D>
 hipError_t launch_tiles(const AttendArgs& a, hipStream_t stream) {
-    const int64_t grid = tile_blocks(a.n_rows, a.g, a.n_seq) * a.n_kv * a.splits;
+    const int64_t grid = a.items * a.n_kv;
     if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
     const int store = a.n_rows > 4096 ? 4 : 1;
     hipLaunchKernelGGL(store_tokens_kernel, dim3((a.n_rows + store - 1) / store), dim3(kThreads),
                        0, stream, a, Lay<kDtype, D>::kRow, store);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((attend_tiles_kernel<kDtype, D>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
-                       a);
+    hipLaunchKernelGGL((attend_tiles_kernel<kDtype, D>), dim3((unsigned)grid), dim3(kThreads), 0,
+                       stream, a);
     return hipGetLastError();
 }
 
@@ -609,41 +658,40 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
     // registers.)
     pl.tiled = (groups >= (p.dtype == STAR_BF16 ? 112 : 160) || (groups >= 56 && keys >= 4096)) &&
                !(p.dtype == STAR_F32 && p.head_dim == 256);
-    pl.splits = 1;
-    const int64_t most = tile_blocks(p.n_rows, g, p.n_seq) * p.n_kv_heads;
-    if (pl.tiled && most <= kMaxTickets) {
-        int splits = 1;
-        if (2 * groups <= kPlaces) {
-            // Places stay free: each block's keys are cut, into parts that pay from
-            // sixteen tiles each (512 rows after 16000 tokens: 416 -> 172 us; after
-            // 512, two parts of eight tiles: 38 -> 43)
-            pl.part_tiles = 16;
-            splits = (int)(kPlaces / groups);
-        } else {
-            // Cut keys fill the last round of places better, for 4% of a round a
-            // cut; a round that leaves every CU one workgroup takes 0.62 of one.
-            // Worth it for long parts (300 workgroups over 9200 tokens: 300 -> 225
-            // us; 520: 464 -> 384; 700: 512 against 532; 640 over a window of 4096:
-            // 205 against 229)
-            pl.part_tiles = 40;
-            auto cost = [&](int s) {
-                const double rounds = (double)groups * s / kPlaces, part = rounds - (int)rounds;
-                return ((int)rounds + (part > 0.5 ? 1.0 : part > 0.0 ? 0.62 : 0.0)) / s +
-                       0.04 * (s - 1);
-            };
-            for (int s = 2; s <= 3; ++s)
-                if (cost(s) < 0.93 * cost(1) && cost(s) < cost(splits)) splits = s;
-        }
-        // (no more than the most keys could use: workgroups that find nothing to do
-        // crowd the others' CUs, 38 -> 45 us for 512 rows after 512 tokens)
-        const int tile = p.head_dim * e > 256 ? 32 : 64;
-        pl.splits = (int)std::max<int64_t>(
-            1, std::min<int64_t>(splits, keys / tile / pl.part_tiles));
+    if (!pl.tiled) return;
+    const int64_t most = tile_blocks(p.n_rows, g, p.n_seq);
+    const int64_t key_tiles = keys / (p.head_dim * e > 256 ? 32 : 64);
+    int splits = 1;
+    pl.part_tiles = kPartTiles;
+    if (2 * groups <= kPlaces) {
+        // Places stay free: each block's keys are cut, into parts that pay from
+        // sixteen tiles each (512 rows after 16000 tokens: 416 -> 172 us; after
+        // 512, two parts of eight tiles: 38 -> 43)
+        splits = (int)std::min<int64_t>(kMaxParts, kPlaces / groups);
+    } else {
+        // Cut keys fill the last round of places better, for 4% of a round a
+        // cut; a round that leaves every CU one workgroup takes 0.62 of one.
+        // Worth it for long parts (300 workgroups over 9200 tokens: 300 -> 225
+        // us; 520: 464 -> 384; 700: 512 against 532; 640 over a window of 4096:
+        // 205 against 229)
+        pl.part_tiles = 40;
+        auto cost = [&](int s) {
+            const double rounds = (double)groups * s / kPlaces, last = rounds - (int)rounds;
+            return ((int)rounds + (last > 0.5 ? 1.0 : last > 0.0 ? 0.62 : 0.0)) / s +
+                   0.04 * (s - 1);
+        };
+        for (int s = 2; s <= 3; ++s)
+            if (cost(s) < 0.93 * cost(1) && cost(s) < cost(splits)) splits = s;
     }
-    if (pl.tiled)
-        pl.part_bytes = pl.splits == 1 ? 0
-                                       : (size_t)most * pl.splits * (p.head_dim / 2 + 4) *
-                                             kThreads * sizeof(float);
+    // (no more than the most keys could use)
+    if (most * p.n_kv_heads <= kMaxTickets)
+        pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, key_tiles / pl.part_tiles));
+    // (and parts of blocks that are longer than others)
+    pl.items = most * pl.splits;
+    if (pl.splits > 1 && p.n_seq <= 64) pl.items += kMoreParts / p.n_kv_heads;
+    pl.part_bytes = pl.splits == 1 ? 0
+                                   : (size_t)(pl.items * p.n_kv_heads) * (p.head_dim / 2 + 4) *
+                                         kThreads * sizeof(float);
 }
 
 hipError_t launch_attend_tiles(const AttendArgs& a, int dtype, int head_dim, hipStream_t stream) {

@@ -186,16 +186,17 @@ struct AttendArgs {
     int ps_log2, n_pages, max_pages, window, sinks;
     float scale_log2;           // scale * log2(e)
     int min_steps;
-    int splits, part_tiles;     // the tiled kernel: parts of a block's keys at most, and
-                                // the fewest tiles of one
+    int splits, part_tiles;     // the tiled kernel: parts that a block's keys are cut into
+                                // where this leaves each so many tiles,
+    int64_t items;              // and the workgroups of a key-value head
 };
 struct AttendPlan {
     int grid = 0;               // workgroups of the row-block kernel
     int min_steps = 1;          // steps that a workgroup takes at least
     size_t part_bytes = 0;
     bool tiled = false;         // the kernel of attend_prompt.hip
-    int splits = 1;             // the most parts it cuts a block's keys into,
-    int part_tiles = 16;        // of this many tiles at least
+    int splits = 1, part_tiles = 16;        // see AttendArgs
+    int64_t items = 0;
 };
 // whether and how attend_prompt.hip's kernel takes a call
 void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl);

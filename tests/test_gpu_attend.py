@@ -366,6 +366,21 @@ def test_prompt_tiled_cut_keys(Hq, Hkv, D, T, past, window, sinks, dtype):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])   # no order of arrival in it
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,window,sinks,dtype", [
+    (32, 32, 64, 0, 0, "bf16"), (40, 20, 128, 0, 0, "bf16"), (32, 32, 64, 3000, 70, "bf16"),
+    (24, 24, 64, 0, 0, "f32"), (28, 28, 128, 0, 0, "f32"), (16, 16, 256, 0, 0, "bf16")])
+def test_prompt_tiled_longer_blocks_are_cut(Hq, Hkv, D, window, sinks, dtype):
+    """One launch of requests after long, middling and no prefixes: as many workgroups
+    as a block's keys ask for."""
+    new = [300, 200, 0, 100, 150]
+    past = [4000, 100, 6000, 2500, 0]
+    c = Cache(11, [n + m for n, m in zip(new, past)], new, Hq, Hkv, D, dtype, ps=64, peak=3.0)
+    assert tiled(c) and star.attend_prompt_workspace_size(c.params(0, 0)) > 1 << 20
+    a = check(c, False, window, sinks)
+    b = run(c, False, window, sinks)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (64, 0), (100, 70), (128, 1),
                                           (2 ** 31 - 1, 3), (500, 2 ** 31 - 1)])
 def test_prompt_windows(window, sinks):
