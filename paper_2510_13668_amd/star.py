@@ -224,11 +224,12 @@ def _arrays(dev: int, wants, *ts):
     return out
 
 
-def _stream(stream) -> int:
-    """The hipStream_t of `stream`, or of the current device's current stream."""
+def _stream(stream, dev=None) -> int:
+    """The hipStream_t of `stream`, or of the current device's (dev, where the
+    caller knows it) current stream."""
     if stream is None:
         if _raw_current_stream is not None:
-            return _raw_current_stream(torch.cuda.current_device())
+            return _raw_current_stream(torch.cuda.current_device() if dev is None else dev)
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -479,7 +480,7 @@ def assign_pages(p: PagesParams, parent, new_len, inst_of, table, seq_len, seq_i
     _check("star_assign_pages", lib().star_assign_pages(
         ctypes.byref(p), parent, new_len, inst_of, table, seq_len, seq_inst, refs,
         _pool(kv, pool), table_out, seq_len_out, seq_inst_out, refs_out,
-        ws.ptr, ws.nbytes, _stream(stream)))
+        ws.ptr, ws.nbytes, _stream(stream, dev)))
 
 
 def compact_pages_workspace_size(p: PagesParams) -> int:
@@ -496,7 +497,7 @@ def compact_pages(p: PagesParams, table, seq_len, refs, kv, table_out, refs_out,
         table, seq_len, refs, table_out, refs_out, n_live)
     _check("star_compact_pages", lib().star_compact_pages(
         ctypes.byref(p), table, seq_len, refs, _pool(kv, pool), table_out, refs_out, n_live,
-        ws.ptr, ws.nbytes, _stream(stream)))
+        ws.ptr, ws.nbytes, _stream(stream, dev)))
 
 
 # ---------------------------------------------------------------------------
@@ -573,7 +574,7 @@ def attend_decode(p: AttendParams, q, k_new, v_new, kv, table, seq_len, out, lse
     _check("star_attend_decode", lib().star_attend_decode(
         ctypes.byref(p),
         *_attend_ptrs(p, q, k_new, v_new, kv, table, seq_len, (), out, lse, dev),
-        ws.ptr, ws.nbytes, _stream(stream)))
+        ws.ptr, ws.nbytes, _stream(stream, dev)))
 
 
 def attend_prompt_workspace_size(p: AttendParams) -> int:
@@ -589,4 +590,4 @@ def attend_prompt(p: AttendParams, q, k_new, v_new, kv, table, seq_len, q_start,
     _check("star_attend_prompt", lib().star_attend_prompt(
         ctypes.byref(p),
         *_attend_ptrs(p, q, k_new, v_new, kv, table, seq_len, (q_start,), out, lse, dev),
-        ws.ptr, ws.nbytes, _stream(stream)))
+        ws.ptr, ws.nbytes, _stream(stream, dev)))
