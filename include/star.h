@@ -445,9 +445,14 @@ typedef struct {
  * tokens are those of slot a = parent[b] (b itself if parent is NULL; -1:
  * none, keep = 0).  Of their pages,
  *   - on the same instance the full ones become shared with a (each further
- *     row that holds a page adds 1 to its count), and the partly filled one is
- *     kept where a == b and its count is 1, else copied, so that the tokens to
- *     come never go to a shared page;
+ *     row that holds a page adds 1 to its count).  Two are not, the partly
+ *     filled one, and that of the last token of a slot that is cut
+ *     (a == b, new_len < seq_len) or of a fork (a != b) that does not grow: they
+ *     are kept where a == b, the count is 1 and no other slot of the call has
+ *     the page among those it shares, served or not, else copied.  So neither the
+ *     tokens to come nor the last one, written anew, go to a shared page, unless
+ *     the slot keeps its length: its pages stay, shared or not, and it has to grow
+ *     before attention stores for it;
  *   - on another instance all are copied.
  * Copies and further pages take the instance's pages that are free on entry,
  * ascending, slots and then page positions ascending.  Pages given up serve

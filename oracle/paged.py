@@ -29,10 +29,26 @@ def assign(table, seq_len, seq_inst, refs, kv, new_len, parent=None, inst_of=Non
     free = [[x for x in range(i * P, (i + 1) * P) if R[x] == 0] for i in range(n_inst)]
     run, flags = [0] * n_inst, 0
     fine = lambda x: 0 <= x < n_pages
+    source = lambda b: b if parent is None else int(parent[b])
+    target = lambda b: I[b] if inst_of is None else int(inst_of[b])
+
+    def whole(b):
+        """Pages of its source that slot b may share in any case: full ones, and in
+        a fork or a cut not that of its last token."""
+        a, want = source(b), int(new_len[b])
+        if a != b or want < L[a]:
+            return max(0, min(want - 1, L[a]) // ps)
+        return L[a] // ps
+
+    taken = [0] * n                    # pages of a slot that forks share
+    for c in range(n):
+        a = source(c)
+        if (0 <= a < n and a != c and 0 <= int(new_len[c]) <= M * ps and
+                all(0 <= L[x] <= M * ps and 0 <= I[x] < n_inst for x in (a, c)) and
+                I[a] == target(c)):
+            taken[a] = max(taken[a], whole(c))
     for b in range(n):
-        a = b if parent is None else int(parent[b])
-        want = int(new_len[b])
-        to = I[b] if inst_of is None else int(inst_of[b])
+        a, want, to = source(b), int(new_len[b]), target(b)
         ok = True
         if not (0 <= L[b] <= M * ps and 0 <= want <= M * ps):
             ok, flags = False, flags | BAD_LEN
@@ -50,8 +66,9 @@ def assign(table, seq_len, seq_inst, refs, kv, new_len, parent=None, inst_of=Non
         keep = min(want, L[a]) if a >= 0 else 0
         shared = 0
         if a >= 0 and I[a] == to:
-            shared = keep // ps
-            if keep % ps and a == b and fine(t_in[b][shared]) and R[t_in[b][shared]] == 1:
+            shared = whole(b)
+            if (a == b and shared * ps < keep and fine(t_in[b][shared]) and
+                    R[t_in[b][shared]] == 1 and taken[b] <= shared):
                 shared += 1
         kept, pages, old = _ceil(keep, ps), _ceil(want, ps), _ceil(L[b], ps)
         need = pages - shared

@@ -52,13 +52,28 @@ struct AssignArgs {
     int32_t* free_list;   // [n_inst][P]
     int32_t* copies;      // [n_inst][P][2] (source, target)
     int32_t* n_copies;    // [n_inst]
+    int32_t* taken;       // [n_seq]: pages of a slot that forks share (cut slots alone)
     int32_t* err;
     int n_seq, max_pages, n_pages, n_inst, ps_log2, n_layers;
     int64_t page_bytes, page_stride, layer_stride;
 };
 
-// One slot's demand, from its arrays alone.
-__device__ inline SlotPlan plan_slot(const AssignArgs& a, int b, int& need, int32_t& bad) {
+// The counts that forks leave for the slots they share pages of are set, raised
+// and read by one workgroup's threads, past the caches.
+__device__ inline void taken_set(int32_t* x) {
+    __hip_atomic_store(x, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline void taken_raise(int32_t* x, int pages) {
+    __hip_atomic_fetch_max(x, pages, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline int taken_read(const int32_t* x) {
+    return __hip_atomic_load(x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// One slot's demand, from its arrays, and where a cut slot keeps its last page
+// (cut), from what forks of this call take of it (taken; null: nothing).
+__device__ inline SlotPlan plan_slot(const AssignArgs& a, int b, const int32_t* taken, int& need,
+                                     bool& cut, int32_t& bad) {
     SlotPlan s;
     const int ps = 1 << a.ps_log2, most = a.max_pages << a.ps_log2;
     const int len = a.seq_len[b], want = a.new_len[b];
@@ -71,6 +86,7 @@ __device__ inline SlotPlan plan_slot(const AssignArgs& a, int b, int& need, int3
         ok = false, bad |= STAR_DEV_BAD_INST;
     if (from < -1 || from >= a.n_seq) ok = false, bad |= STAR_DEV_BAD_PARENT;
     int keep = 0, shared = 0;
+    cut = false;
     if (ok && from >= 0) {
         int from_len = len, from_inst = inst;
         if (from != b) {
@@ -81,11 +97,17 @@ __device__ inline SlotPlan plan_slot(const AssignArgs& a, int b, int& need, int3
         }
         keep = min(want, ok ? from_len : 0);
         if (ok && from_inst == to) {
-            shared = keep >> a.ps_log2;
-            // the page that the next tokens go into has to be the slot's alone
-            if ((keep & (ps - 1)) && from == b) {
+            // The page that the next tokens go into has to be the slot's alone, and
+            // so has that of the last token where attention may store it anew before
+            // the slot grows: after a cut, and in a fork
+            const bool anew = from != b || want < from_len;
+            shared = max(0, anew ? min(want - 1, from_len) : from_len) >> a.ps_log2;
+            if (from == b && shared << a.ps_log2 < keep) {
                 const int last = a.table[(int64_t)b * a.max_pages + shared];
-                if ((uint32_t)last < (uint32_t)a.n_pages && a.refs[last] == 1) ++shared;
+                if ((uint32_t)last < (uint32_t)a.n_pages && a.refs[last] == 1) {
+                    cut = anew;
+                    if (!(cut && taken && taken_read(taken + b) > shared)) ++shared;
+                }
             }
         }
     }
@@ -138,11 +160,38 @@ __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a)
     SlotPlan slot0 = {};
     slot0.inst = -1;
     int64_t mine = 0, copying = 0;
-    for (int b = b0; b < b1; ++b) {
-        int need;
-        const SlotPlan s = plan_slot(a, b, need, bad);
-        if (b == b0) slot0 = s, need0 = need;
-        if (s.inst == inst) mine += need, copying += s.kept - s.shared;
+    const int32_t* taken = nullptr;
+    bool cuts = false, cut;
+    auto demands = [&]() {
+        mine = copying = 0;
+        for (int b = b0; b < b1; ++b) {
+            int need;
+            const SlotPlan s = plan_slot(a, b, taken, need, cut, bad);
+            if (b == b0) slot0 = s, need0 = need;
+            if (s.inst == inst) mine += need, copying += s.kept - s.shared, cuts |= cut;
+        }
+    };
+    demands();
+    if (a.parent && __syncthreads_or(cuts)) {
+        // a cut slot's last page may be one that a fork takes as a full one: the
+        // forks say how many pages they share before the demands count
+        for (int b = b0; b < b1; ++b) {
+            int need;
+            if (plan_slot(a, b, nullptr, need, cut, bad).inst == inst && cut)
+                taken_set(a.taken + b);
+        }
+        xch_wait_stores();
+        __syncthreads();
+        for (int b = b0; b < b1; ++b) {
+            int need;
+            const SlotPlan s = plan_slot(a, b, nullptr, need, cut, bad);
+            if (s.inst == inst && s.from >= 0 && s.from != b && s.shared)
+                taken_raise(a.taken + s.from, s.shared);
+        }
+        xch_wait_stores();
+        __syncthreads();
+        taken = a.taken;
+        demands();
     }
 
     // the instance's free pages in order: each wave counts its stretch, then
@@ -188,7 +237,7 @@ __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a)
         SlotPlan s = slot0;
         if (b < b1) {
             int need = need0;
-            if (i > 0) s = plan_slot(a, b, need, bad);
+            if (i > 0) s = plan_slot(a, b, taken, need, cut, bad);
             if (s.inst == inst) {
                 s.first = (int)min(upto, (int64_t)P);
                 upto += need;
@@ -465,6 +514,7 @@ PagesPlan plan_pages(const star_pages_params& p) {
     pl.copies_off = take((size_t)p.n_pages * 8);
     pl.list_off = take((size_t)p.n_pages * 4);           // free pages, or the page map
     pl.slots_off = take((size_t)p.n_seq * kSlotPlanBytes);
+    pl.taken_off = take((size_t)p.n_seq * 4);
     pl.total = at;
     return pl;
 }
@@ -483,6 +533,7 @@ hipError_t launch_assign(const star_pages_params& p, const PagesPlan& pl, const 
     a.free_list = (int32_t*)(ws + pl.list_off);
     a.copies = (int32_t*)(ws + pl.copies_off);
     a.n_copies = (int32_t*)(ws + pl.n_copies_off);
+    a.taken = (int32_t*)(ws + pl.taken_off);
     a.err = (int32_t*)(ws + kHdrErrorWord);
     a.n_seq = p.n_seq, a.max_pages = p.max_pages, a.n_pages = p.n_pages, a.n_inst = p.n_inst;
     a.ps_log2 = __builtin_ctz(p.page_size), a.n_layers = p.n_layers;

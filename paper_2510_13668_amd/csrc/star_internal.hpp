@@ -158,7 +158,8 @@ hipError_t launch_plan(const star_plan_params& p, const PlanPlan& pl, const int3
 // Pages of the cache (pages.hip): offsets in the workspace.
 constexpr size_t kSlotPlanBytes = 32;
 struct PagesPlan {
-    size_t n_copies_off = 0, copies_off = 0, list_off = 0, slots_off = 0, total = 0;
+    size_t n_copies_off = 0, copies_off = 0, list_off = 0, slots_off = 0, taken_off = 0,
+           total = 0;
 };
 PagesPlan plan_pages(const star_pages_params& p);
 hipError_t launch_assign(const star_pages_params& p, const PagesPlan& pl, const int32_t* parent,
