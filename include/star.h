@@ -503,9 +503,10 @@ star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
  * and gives
  *     out = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j exp(scale q . k_j)
  * (natural logarithm; 0 and -infinity where nothing is visible, or every
- * visible score is -infinity).  What a row does not see does not change it,
- * whatever it holds; pages that no row sees
- * are not read, and their table entries mean nothing.
+ * visible score is -infinity).  A value that is not finite leaves its column of the
+ * rows that see it infinite or NaN (infinity times a weight that has run down to 0
+ * is no number).  What a row does not see does not change it, whatever it holds;
+ * pages that no row sees are not read, and their table entries mean nothing.
  *   Both calls first store the new tokens: k_new and v_new are the keys and
  * values of the last tokens of each request, which seq_len counts already
  * (star_assign_pages made room).  The page that a request's new tokens go to

@@ -1,8 +1,7 @@
 """Plain restatement of the paged cache's operators -- TEST INFRASTRUCTURE.
 
 Page tables: one slot and one page after the other, in order.  Attention: one
-request after the other over its tokens in a plain row, in 64 bits, row by row
-where some are not finite.  Host tensors in and out; nothing here imports the HIP
+request after the other over its tokens in a plain row, in 64 bits.  Host tensors in and out; nothing here imports the HIP
 path.
 """
 from __future__ import annotations
@@ -191,26 +190,27 @@ def attend(q, k_new, v_new, kv, table, seq_len, q_start=None, *, scale, window=0
 
         # query head h reads key-value head h // g
         kg, vg = (t.repeat_interleave(g, dim=0) for t in (k, v))
-        finite = bool(torch.isfinite(k).all() and torch.isfinite(v).all())
-        for at in range(0, T, 64 if finite else 1):
-            rows = slice(lo + at, lo + min(T, at + (64 if finite else 1)))
+        # values that are not finite reach the rows that see them, as by a positive weight
+        odd = ~torch.isfinite(vg)
+        vf = vg.masked_fill(odd, 0.0)
+        for at in range(0, T, 64):
+            rows = slice(lo + at, lo + min(T, at + 64))
             pos = torch.arange(L - T + at, L - T + at + rows.stop - rows.start)
             see = torch.stack([visible(int(p)) for p in pos])          # [rows, L]
-            if finite:
-                kh, vh = kg, vg
-            else:                                    # one row, over the keys it sees
-                kh, vh, see = kg[:, see[0]], vg[:, see[0]], see[:, see[0]]
             qh = q[rows].double().transpose(0, 1)                      # [Hq, rows, D]
-            z = (scale * (qh @ kh.transpose(1, 2))).masked_fill(~see, -math.inf)
-            if see.shape[1] == 0:
-                continue
+            z = (scale * (qh @ kg.transpose(1, 2))).masked_fill(~see, -math.inf)
             top = z.max(dim=2).values
             e = torch.exp(z - top.clamp(min=-1e300)[..., None])
             total = e.sum(2)
             pr = e / total.clamp(min=1e-300)[..., None]
-            out[rows] = (pr @ vh).transpose(0, 1)
-            mass[rows] = (pr @ vh.abs()).transpose(0, 1)
+            o = pr @ vf
+            if odd.any():
+                for x, here in ((math.inf, vg == math.inf), (-math.inf, vg == -math.inf),
+                                (math.nan, torch.isnan(vg))):
+                    o = torch.where(see.double() @ here.double() > 0, o + x, o)
+            out[rows] = o.transpose(0, 1)
+            mass[rows] = (pr @ vf.abs()).transpose(0, 1)
             lse[rows] = (top + torch.log(total)).transpose(0, 1)
-            span = (abs(scale) * (qh.abs() @ kh.abs().transpose(1, 2))).masked_fill(~see, 0.0)
+            span = (abs(scale) * (qh.abs() @ kg.abs().transpose(1, 2))).masked_fill(~see, 0.0)
             reach[rows] = span.max(dim=2).values.transpose(0, 1)
     return dict(out=out, lse=lse, written=written, mass=mass, reach=reach, kv=kv_out, flags=flags)
