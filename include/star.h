@@ -512,8 +512,13 @@ star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
  * (star_assign_pages made room).  The page that a request's new tokens go to
  * must be its alone.
  *   Precision: bf16 or fp32 operands, fp32 scores, softmax statistics and
- * sums; the probabilities enter the second product as a bf16 hi/lo pair or as
- * one bf16 (long prompts) for bf16, as fp32 for fp32; one rounding of out.
+ * sums; the probabilities enter the second product as fp32 for fp32, as a bf16
+ * hi/lo pair for bf16 (2^-16 of each), or as one bf16 (2^-8 of each) in bf16
+ * calls of star_attend_prompt with many rows: those of
+ *     n_kv_heads ((n_rows n_heads / n_kv_heads + 64 n_seq) / 128)   (a whole quotient)
+ * >= 112, or >= 56 where rows can see 4096 keys (max_pages page_size, under a
+ * window at most window + sinks).  That goes by the parameters alone, not by
+ * lengths or by the other requests' rows.  One rounding of out.
  *   A request whose length or row range is out of range is left out, its rows
  * of out and lse stay as they were (STAR_DEV_BAD_LEN); the tokens of a page
  * index out of range are left out (STAR_DEV_BAD_PAGE).

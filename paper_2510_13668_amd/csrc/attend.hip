@@ -119,8 +119,8 @@ __device__ inline f32x4 scores(const u32x4* k, const u32x4* q) {
 }
 
 // O^T += V^T P^T for one tile; p[4 h + x] = lane (r, c)'s token 4c + x of half h.
-// bf16: P enters as a bf16 pair hi + lo (about 2^-17 relative): the products
-// are idle behind the loads, and one bf16 would add its 2^-9 to the output's.
+// bf16: P enters as a bf16 pair hi + lo (2^-16 relative): the products are
+// idle behind the loads, and one bf16 would add its 2^-8 to the output's.
 template <int kDtype, int D>
 __device__ inline void accumulate(const uint32_t (&v)[Tile<kDtype, D>::kRowsV]
                                                      [Tile<kDtype, D>::kRowV / 4],

@@ -12,7 +12,9 @@ namespace {
 
 constexpr int kBM = 128;         // query rows of a workgroup, 32 a wave
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kPlaces = 512;     // workgroups that run at once, two a CU
+// workgroups that run at once, two a CU: the 128-wide and fp32 kernels' (64 wide in
+// bf16 three fit, 256 wide one)
+constexpr int kPlaces = 512;
 constexpr int kMaxParts = 8;     // parts of a block's keys at most
 constexpr int kMoreParts = 512;  // of a launch's longer blocks, beside those the host counts
 constexpr int kPartTiles = 16;   // and the fewest tiles of one: shorter ones do not pay
@@ -88,7 +90,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
     const int head = blockIdx.x % a.n_kv, item = blockIdx.x / a.n_kv;
     int b, block, nth, part = 0, parts = 1;
     if (a.n_seq <= 64) {
-        // one request a lane, every wave by itself
+        // One request a lane, every wave by itself.  More requests run in reverse order,
+        // with one number of parts: that takes 64 unlike chunks after up to 3000 tokens
+        // from 164 to 189 us, 60 of 40 tokens after up to 8000 from 161 to 207, one prompt
+        // of 2000 among 63 of 20 from 83 to 91, and 64 equal prompts of 300 from 226 to 212
         int32_t bad = 0;
         Slot s = {0, 0, 0, 0, 0};
         if (lane < a.n_seq) s = slot_of<kBN>(a, lane, bad);
@@ -409,6 +414,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_tiles_kerne
         }
         const float ref = m == -INFINITY ? 0.0f : m;      // nothing seen yet: all p are 0
         if constexpr (kBf16) {
+            // One bf16 each, half a step (2^-8) off at most: the products share the time with
+            // the softmax, and a hi + lo pair would double the second (8191 tokens
+            // 610 -> 791 us, ragged prompts 323 -> 402; outputs then 1.65e-3 off instead
+            // of 2.2e-3, 1.65e-3 of it their own rounding)
             u32x4 p[kBN / 16];            // 16 tokens each, as the second product takes them
 #pragma unroll
             for (int t = 0; t < kBN / 32; ++t)
@@ -650,12 +659,22 @@ void plan_attend_tiles(const star_attend_params& p, AttendPlan& pl) {
     const int64_t groups = (rows + (int64_t)p.n_seq * kBM / 2) / kBM * p.n_kv_heads;
     int64_t keys = (int64_t)p.max_pages * p.page_size;
     if (p.window) keys = std::min(keys, (int64_t)p.window + p.sinks);
+    // Only the host's numbers decide, so that a captured call keeps its kernel: the
+    // table's width stands for the lengths, and n_rows / n_seq for a request's rows.
+    // What that costs, both kernels measured: calls of single tokens, whose blocks hold
+    // few rows, would be faster by row blocks (124 requests after up to 4000 tokens
+    // 249 us against 211, 31 of them 71 against 56, with 16 heads of their own keys 127
+    // against 158), as star_attend_decode takes them; but slots without rows and single
+    // tokens beside a prompt look the same from here and lose more there (30 single
+    // tokens and 2048 rows of one prompt 121 against 724, 256 and 512 rows 253 against
+    // 342).
     // Fewer workgroups leave the row-block kernel ahead, whose pieces are finer.
     // bf16: 10 prompts of 23 tokens (104) 14.5 us against 13.8, of 70 (64) 14.6 against
     // 17.1, 15 of 27 (56) 9.4 against 13.7; fp32: 26 against 29 at 131, 39 against 35 at
     // 176; a few rows after thousands of tokens, whose keys are cut below, 105
-    // against 50 at 64.  (256 wide in fp32, queries and output alone fill the
-    // registers.)
+    // against 50 at 64 (a table of 4096 tokens whose requests are short gives those
+    // of 56 to 111 the slower side of the figures before).  (256 wide in fp32,
+    // queries and output alone fill the registers.)
     pl.tiled = (groups >= (p.dtype == STAR_BF16 ? 112 : 160) || (groups >= 56 && keys >= 4096)) &&
                !(p.dtype == STAR_F32 && p.head_dim == 256);
     if (!pl.tiled) return;
