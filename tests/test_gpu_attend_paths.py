@@ -1,4 +1,5 @@
-"""Which kernel takes a prompt call, and what precision it has there."""
+"""Which kernel takes a prompt call, what precision it has there, and the paths of
+cut keys that lengths, windows and many requests open."""
 import pytest
 import torch
 
@@ -64,6 +65,32 @@ def test_a_window_narrows_the_keys_that_rows_can_see():
         check(c, False, window, sinks)
 
 
+def cut(c, window=0, sinks=0):
+    """The call holds room for parts of cut blocks."""
+    assert tiled(c)
+    assert star.attend_prompt_workspace_size(c.params(window, sinks)) > 1 << 20
+    a = check(c, False, window, sinks)
+    b = run(c, False, window, sinks)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])   # no order of arrival in it
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,T,past,window,sinks,dtype", [
+    (32, 16, 128, 450, 2600, 2100, 9, "bf16"), (16, 16, 64, 900, 2900, 2300, 0, "bf16"),
+    (28, 28, 256, 490, 1500, 1100, 5, "bf16"), (24, 24, 64, 900, 2800, 2500, 3, "f32"),
+    (48, 24, 128, 450, 2000, 1600, 70, "f32")])
+def test_keys_cut_under_a_window(Hq, Hkv, D, T, past, window, sinks, dtype):
+    cut(Cache(6, [past + T], [T], Hq, Hkv, D, dtype, ps=64, peak=3.0), window, sinks)
+
+
+@pytest.mark.parametrize("Hkv,D,dtype", [(2, 64, "bf16"), (3, 64, "f32"), (2, 128, "bf16")])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2200, 7)])
+def test_keys_cut_of_more_than_64_requests(Hkv, D, dtype, window, sinks):
+    new = [70 + b % 5 for b in range(70)]
+    past = [3000 * (b * 7 % 23) // 22 for b in range(70)]
+    lens = [n + m for n, m in zip(new, past)]
+    cut(Cache(8, lens, new, Hkv, Hkv, D, dtype, ps=64, peak=3.0), window, sinks)
+
+
 def test_single_tokens_beside_a_chunk():
     new = [1] * 40 + [300] + [1] * 40
     lens = [1 + 29 * b % 200 for b in range(40)] + [900] + [1 + 31 * b % 150 for b in range(40)]
@@ -83,3 +110,28 @@ def test_a_table_wider_than_its_requests():
         d.table = torch.cat([d.table, torch.full((4, 300), 10 ** 6, dtype=torch.int32)], dim=1)
         d.M = d.table.shape[1]
         check(d, True)
+
+
+def test_an_error_is_kept_until_it_is_read():
+    """Calls of either kind between do not lose it, the read clears it."""
+    ws = star.Workspace(1 << 25)
+
+    def call(c, decode):
+        p, (q, k, v) = c.params(0, 0), c.split(c.qkv.to("cuda"))
+        out = torch.empty((c.qkv.shape[0], c.Hq, c.D), dtype=c.qkv.dtype, device="cuda")
+        args = [t.to("cuda") for t in (c.kv, c.table, c.len)]
+        if decode:
+            star.attend_decode(p, q, k, v, *args, out, None, ws)
+        else:
+            star.attend_prompt(p, q, k, v, *args, c.start.to("cuda"), out, None, ws)
+
+    good = Cache(16, [3000, 5], [1, 1], 4, 1, 64), Cache(17, [300], [300], 4, 1, 64)
+    short, page = Cache(16, [40, 5], [1, 1], 4, 1, 64), Cache(17, [60], [50], 4, 1, 64)
+    short.len[1], page.table[0, 1] = -1, -1
+    for bad, decode, flag in ((short, True, star.DEV_BAD_LEN), (page, False, star.DEV_BAD_PAGE)):
+        call(bad, decode)
+        call(good[0], True)
+        call(good[1], False)
+        assert ws.read_device_error() == flag
+        call(good[0], True)
+        assert ws.read_device_error() == 0
