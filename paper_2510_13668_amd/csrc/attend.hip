@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
 
     // this workgroup's piece of the other blocks' steps
     const int64_t total = s_steps[kThreads] - n_short;
-    const int64_t piece = max((int64_t)a.min_steps, quotient(total + gridDim.x - 1, gridDim.x));
+    const int64_t piece = max((int64_t)1, quotient(total + gridDim.x - 1, gridDim.x));
     int64_t u = wg * piece;
     const int64_t end = min(total, u + piece);
     int64_t k = wg + (int64_t)wave * gridDim.x;          // this wave's next one-step block
@@ -677,7 +677,6 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     // two workgroups a CU (one where a row's 256 elements fill the registers)
     pl.grid = p.head_dim == 256 ? 256 : 512;
     static_assert(512 <= kMaxTickets, "one ticket per workgroup");
-    pl.min_steps = 1;
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
     if (!decode) plan_attend_tiles(p, pl);
     return pl;
@@ -686,7 +685,6 @@ AttendPlan plan_attend(const star_attend_params& p, bool decode) {
 hipError_t launch_attend(const AttendPlan& pl, const AttendArgs& args, int dtype, int head_dim,
                          hipStream_t stream) {
     AttendArgs a = args;
-    a.min_steps = pl.min_steps;
     a.splits = pl.splits;
     a.part_tiles = pl.part_tiles;
     a.items = pl.items;

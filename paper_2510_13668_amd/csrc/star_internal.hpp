@@ -186,14 +186,12 @@ struct AttendArgs {
     int n_seq, n_rows, n_heads, n_kv, g;        // g: query heads per key-value head
     int ps_log2, n_pages, max_pages, window, sinks;
     float scale_log2;           // scale * log2(e)
-    int min_steps;
     int splits, part_tiles;     // the tiled kernel: parts that a block's keys are cut into
                                 // where this leaves each so many tiles,
     int64_t items;              // and the workgroups of a key-value head
 };
 struct AttendPlan {
     int grid = 0;               // workgroups of the row-block kernel
-    int min_steps = 1;          // steps that a workgroup takes at least
     size_t part_bytes = 0;
     bool tiled = false;         // the kernel of attend_prompt.hip
     int splits = 1, part_tiles = 16;        // see AttendArgs
