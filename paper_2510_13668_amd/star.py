@@ -539,6 +539,8 @@ def _attend_layout(fields: bytes):
     k_new and v_new, and kv, and the (type, bytes) of its other arrays (by value,
     since a dozen reads of a ctypes structure take 1 us of a small call's 8)."""
     p = AttendParams.from_buffer_copy(fields)
+    if p.dtype not in _TORCH_DTYPES:
+        raise ValueError(f"dtype {p.dtype} is neither F32 nor BF16")
     dt, D, n, Hkv, ps = _TORCH_DTYPES[p.dtype], p.head_dim, p.n_rows, p.n_kv_heads, p.page_size
     i32 = torch.int32
     return (dt, (n, p.n_heads, D), (p.q_stride, D, 1), (n, Hkv, D), (p.kv_stride, D, 1),

@@ -221,3 +221,18 @@ def test_attention_of_nothing_launches_nothing(L):
     assert _decode(L, _attend(n_seq=0, n_rows=0)) == 0
     assert _prompt(L, _attend(n_seq=0, n_rows=0)) == 0
     assert _prompt(L, _attend(n_seq=4, n_rows=0)) == 0
+
+
+def test_binding_refuses_types_it_does_not_know(monkeypatch):
+    """A type that is none of the two is a ValueError, as the other mistakes are."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    class At(_Meta):
+        def get_device(self):
+            return 0
+
+    t = At(torch.empty((4, 8, 128), dtype=torch.float16))
+    t.buf = t
+    for call, starts in ((star.attend_decode, ()), (star.attend_prompt, (t,))):
+        with pytest.raises(ValueError):
+            call(_attend(dtype=7), t, t, t, t, t, t, *starts, t, None, t)
