@@ -130,6 +130,7 @@ __device__ inline int stretch_of(int P) {
 
 __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a) {
     __shared__ int s_count[kPlanWaves], s_copies;
+    __shared__ bool s_cuts[kPlanWaves];
     __shared__ int64_t s_tmp[2 * kPlanWaves];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int P = a.n_pages / a.n_inst;
@@ -172,7 +173,34 @@ __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a)
         }
     };
     demands();
-    if (a.parent && __syncthreads_or(cuts)) {
+
+    // the instance's free pages in order: each wave counts its stretch, then
+    // writes it behind the waves before
+    int n = 0;
+    for (int at = from, h = 0; at < to; at += 256, ++h) {
+        int x[4];
+        if (h >= kHeld) load_counts(refs, at, to, lane, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            n += __popcll(__ballot((h == 0 ? held[0][k] : h == 1 ? held[1][k] : x[k]) == 0));
+    }
+    const bool cuts_here = __any(cuts);
+    if (lane == 0) s_count[wave] = n, s_cuts[wave] = cuts_here;
+    int64_t upto, k;
+    auto running = [&]() {
+        upto = mine, k = copying;
+        block_incl_add2_i64<kPlanThreads>(upto, k, s_tmp);
+        upto -= mine, k -= copying;
+    };
+    running();
+    int n_free = 0, rank = 0;
+    bool any_cuts = false;
+    for (int w = 0; w < kPlanWaves; ++w) {
+        if (w < wave) rank += s_count[w];
+        n_free += s_count[w];
+        any_cuts |= s_cuts[w];
+    }
+    if (a.parent && any_cuts) {
         // a cut slot's last page may be one that a fork takes as a full one: the
         // forks say how many pages they share before the demands count
         for (int b = b0; b < b1; ++b) {
@@ -192,26 +220,7 @@ __global__ __launch_bounds__(kPlanThreads) void assign_plan_kernel(AssignArgs a)
         __syncthreads();
         taken = a.taken;
         demands();
-    }
-
-    // the instance's free pages in order: each wave counts its stretch, then
-    // writes it behind the waves before
-    int n = 0;
-    for (int at = from, h = 0; at < to; at += 256, ++h) {
-        int x[4];
-        if (h >= kHeld) load_counts(refs, at, to, lane, x);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            n += __popcll(__ballot((h == 0 ? held[0][k] : h == 1 ? held[1][k] : x[k]) == 0));
-    }
-    if (lane == 0) s_count[wave] = n;
-    int64_t upto = mine, k = copying;
-    block_incl_add2_i64<kPlanThreads>(upto, k, s_tmp);
-    upto -= mine, k -= copying;
-    int n_free = 0, rank = 0;
-    for (int w = 0; w < kPlanWaves; ++w) {
-        if (w < wave) rank += s_count[w];
-        n_free += s_count[w];
+        running();
     }
     int32_t* list = a.free_list + page0;
     for (int at = from, h = 0; at < to; at += 256, ++h) {
