@@ -67,8 +67,8 @@ struct Half {
 };
 
 // A lane's share of a V row.  Values that one block alone reads pass the caches
-// by, whole lines at a time (128 requests: 382 -> 364 us, 6.0 TB/s; two long
-// ones 75.5 -> 67.7; where several blocks read them, 76 -> 93); keys take two
+// by, whole lines at a time (128 requests: 379 -> 362 us, 6.0 TB/s; two long
+// ones 79 -> 77; where several blocks read them, 76 -> 93); keys take two
 // instructions a line, which only the cache joins (the same for them: 364 ->
 // 383).
 template <int kDtype, int D, bool kOnce>
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_rows_kernel
     }
     // Where they fill the chip by themselves, blocks of one step are a wave's
     // each (in batches of short requests three waves of four had no tile, and
-    // every block cost a meeting: 512 requests of 30 tokens took 45 us, now 20)
+    // every block cost a meeting: 512 requests of 30 tokens took 52 us, now 23)
     const int64_t n_short = s_short[kThreads] >= 2 * gridDim.x ? s_short[kThreads] : 0;
     const bool alone_too = n_short > 0;
     // the request that holds step (or one-step block) `at`, and its first
@@ -674,7 +674,8 @@ hipError_t launch_rows(const AttendArgs& a, int grid, hipStream_t stream) {
 
 AttendPlan plan_attend(const star_attend_params& p, bool decode) {
     AttendPlan pl;
-    // two workgroups a CU (one where a row's 256 elements fill the registers)
+    // two workgroups a CU (one where a row's 256 elements fill the registers; 64 wide
+    // a third would fit)
     pl.grid = p.head_dim == 256 ? 256 : 512;
     static_assert(512 <= kMaxTickets, "one ticket per workgroup");
     pl.part_bytes = (size_t)2 * pl.grid * (kRows * p.head_dim + 4 * kRows) * sizeof(float);
