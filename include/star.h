@@ -510,7 +510,8 @@ star_status star_compact_pages(const star_pages_params* p, const int32_t* table,
  *   Both calls first store the new tokens: k_new and v_new are the keys and
  * values of the last tokens of each request, which seq_len counts already
  * (star_assign_pages made room).  The page that a request's new tokens go to
- * must be its alone.
+ * must be its alone: star_assign_pages leaves it so for the tokens that a slot
+ * gains, and for the last one where it was cut or forked.
  *   Precision: bf16 or fp32 operands, fp32 scores, softmax statistics and
  * sums; the probabilities enter the second product as fp32 for fp32, as a bf16
  * hi/lo pair for bf16 (2^-16 of each), or as one bf16 (2^-8 of each) in bf16

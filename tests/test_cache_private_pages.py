@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import paged
+from paper_2510_13668_amd import star
 from test_gpu_cache_flow import Instance, N
 from test_gpu_pages import State, _check_assign
 
@@ -92,6 +93,54 @@ def test_cuts_beside_forks(n, M, P, n_inst, ps, move):
             cuts = dev(np.where(rng.random(n) < 0.5, s.len.numpy() // ps * ps, s.len.numpy()))
             _check_assign(s, cuts)
             _check_assign(s, cuts, in_place=True)
+
+
+@pytest.mark.gpu
+def test_cuts_and_forks_when_pages_run_out():
+    """What has no page for its copy stays as it was."""
+    n, M, P, ps = 60, 6, 110, 16
+    s = State(9, n, M, P, 1, ps, fill=1.0)
+    lens = s.len.numpy().astype(np.int64)
+    parent = np.where(s.rng.random(n) < 0.4, s.rng.integers(0, n, n), np.arange(n))
+    new = np.where(s.rng.random(n) < 0.5, lens[parent] // ps * ps, lens[parent])
+    new[::3] = lens[::3] // 2 // ps * ps
+    parent[::3] = np.arange(n)[::3]
+    dev = lambda a: torch.from_numpy(a.astype(np.int32))
+    ref = _check_assign(s, dev(new), dev(parent))
+    assert ref[5] == paged.NO_PAGES and (ref[1] == dev(new)).any()
+    _check_assign(s, dev(np.where(s.rng.random(n) < 0.5, lens // ps * ps, lens)))
+
+
+@pytest.mark.gpu
+def test_cuts_beside_forks_replayed_from_a_graph():
+    """Whatever an earlier call left in the workspace."""
+    n, M, P, ps = 200, 5, 900, 16
+    s = State(10, n, M, P, 2, ps, fill=0.4)
+    p = s.params()
+    ws = star.Workspace(star.assign_pages_workspace_size(p))
+    d = [x.to("cuda") for x in (s.table, s.len, s.inst, s.refs, s.kv)]
+    out = [d[0].clone(), *(torch.zeros_like(x) for x in d[1:4])]
+    parent, new = torch.zeros_like(d[1]), torch.zeros_like(d[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        star.assign_pages(p, parent, new, None, *d, *out, ws)
+    for seed in range(4):
+        rng = np.random.default_rng(seed)
+        a = np.where(rng.random(n) < 0.4, rng.integers(0, n, n), np.arange(n))
+        lens = s.len.numpy()
+        want = np.where(rng.random(n) < 0.4, lens[a] * rng.random(n), lens[a] + rng.integers(0, 2, n))
+        a, want = (torch.from_numpy(x.astype(np.int32)) for x in (a, np.minimum(want, M * ps)))
+        parent.copy_(a)
+        new.copy_(want)
+        for x, y in zip((*out[:1], d[4]), (s.table, s.kv)):
+            x.copy_(y)
+        g.replay()
+        torch.cuda.synchronize()
+        ref = paged.assign(s.table, s.len, s.inst, s.refs, s.kv, want, a, n_inst=2, page_size=ps)
+        for x, y in zip((*out, d[4]), ref):
+            assert torch.equal(x.cpu(), y)
+        assert ws.read_device_error() == ref[5] == 0
+        torch.rand(1000, device="cuda").sum().item()
 
 
 def _grow(s, slots):
